@@ -319,6 +319,71 @@ int syn_op_attention(syn_model *m, syn_kv *kv, const syn_plan *p, uint32_t layer
 int syn_op_attention_static(syn_model *m, syn_kv *kv, const syn_plan *p, uint32_t layer, const void *q, void *out,
                             void *cuda_stream);
 
+/* ---- projections that are not the library's own: per-head norms, rotations, the append -------- */
+
+/* The step's qkv projection normalises, rotates and appends by itself, in one form (whole heads in halves, no norm of
+ * queries and keys, unscaled frequencies).  For q, k and v that come from elsewhere (a model with norms of its queries and
+ * keys, with another rotation, with adapters) these operations bring them to where syn_op_attention finds them. */
+enum { SYN_TYPE_BF16 = 0, SYN_TYPE_F16 = 1, SYN_TYPE_F32 = 2 };
+enum { SYN_ROPE_HALVES = 0, SYN_ROPE_INTERLEAVED = 1 };
+enum {
+    SYN_ROPE_SCALE_NONE = 0,
+    SYN_ROPE_SCALE_LINEAR = 1, /* f / factor                                                                             */
+    SYN_ROPE_SCALE_BASE = 2,   /* base * factor^(d / (d - 2)) in place of base (d = rotary_dim; unchanged for d = 2)     */
+    SYN_ROPE_SCALE_TURNS = 3,  /* f keep + f / factor (1 - keep), keep = (original_len f / 2 pi - low) / (high - low)
+                                * clamped to [0, 1]                                                                      */
+    SYN_ROPE_SCALE_INDEX = 4   /* the same with keep = 1 - (i - first) / (last - first) clamped: linear in the index between
+                                * those of `high` turns (rounded down) and of `low` turns (rounded up) over original_len */
+};
+/* Pair i of the rotary_dim leading components of a head turns by pos * f_i, f_i = base^(-2 i / rotary_dim) scaled as above:
+ * components (i, i + rotary_dim / 2) in halves, (2 i, 2 i + 1) interleaved; the other components pass through.  amplitude
+ * multiplies cosine and sine; 0 stands for 1, and for 0.1 ln(factor) + 1 with SYN_ROPE_SCALE_INDEX.  rotary_dim: even, 2 to
+ * 256.  low, high, original_len: for the last two scalings only; factor: for all but the first. */
+typedef struct {
+    uint32_t rotary_dim, layout, scaling;
+    double base, factor, original_len, low, high, amplitude;
+} syn_rope_desc;
+typedef struct syn_rope syn_rope; /* HOST memory only: usable on every device, stream and thread */
+/* Errors: SYN_E_INVALID_ARG, SYN_E_OOM.  syn_rope_freqs: f_i [rotary_dim / 2] and the amplitude, to HOST memory. */
+int syn_rope_create(const syn_rope_desc *desc, syn_rope **out);
+void syn_rope_free(syn_rope *r);
+int syn_rope_freqs(const syn_rope *r, double *freqs, double *amplitude);
+
+/* The heads of T tokens: token t, head h at x + t * x_stride + h * head_dim (strides in elements, at least
+ * n_heads * head_dim: the arrays may be slices of one row per token).  DEVICE memory aligned to the element; rows that start
+ * on 16-byte boundaries are read and written in 16-byte accesses.  gain: bf16 [head_dim], multiplied into
+ * x / sqrt(mean x^2 + eps) over the head before it is rotated, or NULL: no norm. */
+typedef struct {
+    const void *x;
+    void *y;
+    const void *gain;
+    int64_t x_stride, y_stride;
+    int32_t n_heads;
+} syn_heads;
+
+/* Norm and rotation of queries and keys (either may be NULL) in one launch: y = R(positions[t]) norm(x), computed in fp32 (the
+ * angles in 64 bits) and rounded once.  rope NULL: the norm alone.  positions: DEVICE int32 [T], any values; may be NULL without
+ * rope.  in_type, out_type: SYN_TYPE_*; out_type is in_type, or SYN_TYPE_F16 (what syn_op_attention takes), which saturates at
+ * +-65504.  head_dim: a multiple of 8, at most 256, at least rotary_dim.  y may be x where strides and element sizes
+ * are equal; otherwise y must not overlap any x.  T = 0 does nothing.  Asynchronous on cuda_stream of the current device.
+ * Errors: SYN_E_INVALID_ARG, SYN_E_CUDA. */
+int syn_op_qk_rope(const syn_rope *rope, const syn_heads *q, const syn_heads *k, const int32_t *positions, int32_t T,
+                   int32_t head_dim, float eps, int32_t in_type, int32_t out_type, void *cuda_stream);
+
+/* Appends the plan's chunks to a layer of the cache: token t's keys are normalised (k->gain), rotated by the token's
+ * position (rope; NULL: they are rotated already) and stored with its values at the token's slot, where syn_op_attention with
+ * the same plan reads them; nothing else of the cache is written.  q (may be NULL): the queries, normalised and rotated in the same launch to
+ * q->y, half precision.  k->y and v->y must be NULL, v->gain too; n_heads those of the model, eps the model's rms_eps.  in_type:
+ * SYN_TYPE_* of q, k and v; the cache's half precision saturates at +-65504.  Asynchronous on cuda_stream; the model's device must be
+ * current.  Errors: SYN_E_INVALID_ARG, SYN_E_CUDA. */
+int syn_op_kv_append(syn_model *m, syn_kv *kv, const syn_plan *p, uint32_t layer, const syn_rope *rope, const syn_heads *q,
+                     const syn_heads *k, const syn_heads *v, int32_t in_type, void *cuda_stream);
+
+/* Where a layer's pages lie: DEVICE half precision [n_pages][n_kv_heads][2][16][head_dim], K before V; the memory belongs to
+ * the cache and ends with it.  For callers that look at, fill or transfer pages themselves, ordered with the
+ * library's calls by their streams.  Errors: SYN_E_INVALID_ARG. */
+int syn_kv_layer(const syn_kv *kv, uint32_t layer, void **pool, int64_t *n_elements);
+
 /* The projection kernel's schedule without a device (tests): how a y[T][N] = x[T][K] w[N][K]^T
  * projection with the given epilogue (0 plain store, 1 QKV, 2 residual update, 3 SwiGLU, 4 lm_head)
  * is cut up on n_sm SMs.  syn_gemm_plan_host fills out[SYN_GEMM_PLAN_FIELDS] = {feature pairs of 256,

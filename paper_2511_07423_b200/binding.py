@@ -63,7 +63,7 @@ EXPORTS = ["syn_model_load", "syn_model_free", "syn_kv_alloc", "syn_kv_free", "s
            "syn_op_attention", "syn_op_attention_static",
            "syn_set_profile", "syn_get_profile", "syn_verify_batch_sampled", "syn_op_sample_verify",
            "syn_gemm_plan_host", "syn_gemm_work_host", "syn_gemm2_plan_host", "syn_gemm2_work_host",
-           "syn_thin_plan_host"]
+           "syn_thin_plan_host", "syn_rope_create", "syn_rope_free", "syn_rope_freqs", "syn_op_qk_rope", "syn_op_kv_append", "syn_kv_layer"]
 SCHED_EXPORTS = ["syn_sched_create", "syn_sched_free", "syn_sched_add_request", "syn_sched_add_verify", "syn_sched_finish",
                  "syn_sched_peek", "syn_sched_commit", "syn_sched_step", "syn_sched_get_stats"]
 
@@ -79,9 +79,12 @@ def load_library() -> C.CDLL:
         lib.syn_strerror.argtypes = [C.c_int]
         lib.syn_last_cuda_error.restype = C.c_char_p
         lib.syn_last_cuda_error.argtypes = []
-        for fn in ("syn_model_free", "syn_kv_free", "syn_plan_free", "syn_sched_free"):
+        for fn in ("syn_model_free", "syn_kv_free", "syn_plan_free", "syn_sched_free", "syn_rope_free"):
             getattr(lib, fn).restype = None
             getattr(lib, fn).argtypes = [C.c_void_p]
+        p, i = C.c_void_p, C.c_int32   # declared once: a call of these takes plain numbers
+        lib.syn_op_qk_rope.argtypes = [p, p, p, p, i, i, C.c_float, i, i, p]
+        lib.syn_op_kv_append.argtypes = [p, p, p, C.c_uint32, p, p, p, p, i, p]
         _LIB = lib
     return _LIB
 
@@ -107,6 +110,10 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> C.c_void_p:
     if stream is None:   # with the index given, torch does not look for it among the visible devices (4 us of a 10 us call)
         stream = torch.cuda.current_stream(torch.cuda.current_device())
     return C.c_void_p(stream.cuda_stream)
+
+
+def _raw_stream(stream: Optional[torch.cuda.Stream], device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 class Model:
@@ -172,6 +179,14 @@ class Model:
         return {KERNEL_CLASSES[i]: (ms[i], cnt[i]) for i in range(n)}
 
 
+class _Pages:
+    """Device memory of a cache, described to torch."""
+
+    def __init__(self, kv: "KVCache", at: int, shape):
+        self.kv = kv
+        self.__cuda_array_interface__ = {"shape": shape, "typestr": "<f2", "data": (at, False), "strides": None, "version": 3}
+
+
 class KVCache:
     """syn_kv_alloc / syn_kv_import / syn_kv_export / syn_kv_free."""
 
@@ -199,6 +214,15 @@ class KVCache:
                                        C.c_int32(n_pos), C.c_void_p(k.data_ptr()), C.c_void_p(v.data_ptr()),
                                        _stream_ptr(stream)), "syn_kv_export")
         return k, v
+
+    def layer_view(self, layer: int) -> torch.Tensor:
+        """syn_kv_layer: the layer's pages as a float16 tensor [n_pages, n_kv_heads, 2 (K, V), 16, head_dim] that shares the
+        cache's memory (writes are seen by the calls that follow on the stream).  The tensor keeps this object alive;
+        it must not be used after close()."""
+        s = self.model.shape
+        at, n = C.c_void_p(), C.c_int64()
+        _check(self._lib.syn_kv_layer(self._h, C.c_uint32(layer), C.byref(at), C.byref(n)), "syn_kv_layer")
+        return torch.as_tensor(_Pages(self, at.value, (self.n_pages, s.n_kv_heads, 2, self.page_size, s.head_dim)))
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h:
@@ -282,6 +306,110 @@ def syn_op_sample_verify(logits: torch.Tensor, chunk_tokens, chunk_offsets, n_un
     return acc, cor
 
 
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "turns": 3, "index": 4}
+_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+class _RopeDesc(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("rotary_dim", "layout", "scaling")] \
+        + [(n, C.c_double) for n in ("base", "factor", "original_len", "low", "high", "amplitude")]
+
+
+class Rope:
+    """syn_rope_create / syn_rope_freqs / syn_rope_free: a rotation of the leading `rotary_dim` components of a head, in
+    halves or interleaved, with its frequencies as they are or scaled ("linear", "base", "turns", "index")."""
+
+    def __init__(self, rotary_dim: int, base: float = 10000.0, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+                 original_len: float = 0.0, low: float = 0.0, high: float = 0.0, amplitude: float = 0.0):
+        self._lib = load_library()
+        self._h = C.c_void_p()
+        self.rotary_dim = rotary_dim
+        if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS or not 0 <= rotary_dim < 2 ** 31:
+            raise SynError(-1, f"Rope: layout {layout!r}, scaling {scaling!r}, rotary_dim {rotary_dim!r}")
+        d = _RopeDesc(rotary_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], base, factor, original_len, low, high, amplitude)
+        _check(self._lib.syn_rope_create(C.byref(d), C.byref(self._h)), "syn_rope_create")
+
+    def frequencies(self):
+        """(angle per position of each pair, float64 [rotary_dim / 2] on the CPU; the factor on cosine and sine)."""
+        f, a = torch.empty(self.rotary_dim // 2, dtype=torch.float64), C.c_double()
+        _check(self._lib.syn_rope_freqs(self._h, C.c_void_p(f.data_ptr()), C.byref(a)), "syn_rope_freqs")
+        return f, a.value
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h:
+            self._lib.syn_rope_free(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class _Heads(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("gain", C.c_void_p), ("x_stride", C.c_int64), ("y_stride", C.c_int64),
+                ("n_heads", C.c_int32)]
+
+
+def _heads(what: str, x: torch.Tensor, y: Optional[torch.Tensor], gain: Optional[torch.Tensor], tokens: int, hd: int, dtype, device: int) -> _Heads:
+    """One operand [tokens, heads, hd] (heads side by side, any distance between tokens), checked; y: its output, in any shape
+    whose rows are a token's heads side by side."""
+    n, st = x.shape, x.stride()
+    if len(n) != 3 or n[0] != tokens or n[2] != hd or x.dtype != dtype or x.get_device() != device:
+        raise SynError(-1, f"{what}: {dtype} [{tokens}, heads, {hd}] on the current device")
+    heads, width = n[1], n[1] * hd
+    if (st[2] != 1 and hd > 1) or (st[1] != hd and heads > 1) or (st[0] < width and tokens > 1):
+        raise SynError(-1, f"{what}: the heads of a token lie side by side")
+    ys = width
+    if y is not None:
+        if y.get_device() != device or y.shape[0] != tokens or y.numel() != tokens * width:
+            raise SynError(-1, f"{what}: an output of {tokens} x {width} elements on the current device")
+        if not y.is_contiguous():
+            if y.dim() != 3 or y.stride(2) != 1 or y.stride(1) != hd:
+                raise SynError(-1, f"{what}: the heads of an output's token lie side by side")
+            ys = y.stride(0) if tokens > 1 else width
+    if gain is not None and (gain.dtype != torch.bfloat16 or gain.numel() != hd or not gain.is_contiguous() or gain.get_device() != device):
+        raise SynError(-1, f"{what}: gains are bfloat16 [{hd}] on the current device")
+    return _Heads(x.data_ptr(), y.data_ptr() if y is not None else None, gain.data_ptr() if gain is not None else None,
+                  st[0] if tokens > 1 else width, ys, heads)
+
+
+def syn_op_qk_rope(rope: Optional[Rope], q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: Optional[torch.Tensor],
+                   q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                   q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
+    """syn_op_qk_rope: per-head norm (where a gain is given) and rotation of q [T, heads, hd] and k [T, kv heads, hd], either of
+    which may be None; slices of one projection's rows are fine.  positions: int32 [T].  The outputs have the inputs' dtype unless
+    q_out / k_out (both, of one dtype) say float16; they may be the inputs themselves.  Returns (q_out, k_out)."""
+    lead = q if q is not None else k
+    if lead is None or lead.dim() != 3 or lead.dtype not in _TYPES:
+        raise SynError(-1, "syn_op_qk_rope: q or k [T, heads, hd], bfloat16, float16 or float32")
+    device = torch.cuda.current_device()
+    T, hd, dt = lead.shape[0], lead.shape[2], lead.dtype
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=k_out.dtype if k is not None and k_out is not None else dt, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=q_out.dtype if q is not None else dt, device=k.device)
+    odt = (q_out if q is not None else k_out).dtype
+    if odt not in _TYPES or (q is not None and k is not None and k_out.dtype != odt):
+        raise SynError(-1, "syn_op_qk_rope: both outputs have the inputs' dtype, or float16")
+    if rope is not None and (positions is None or positions.dtype != torch.int32 or positions.numel() != T or not positions.is_contiguous()
+                             or positions.get_device() != device):
+        raise SynError(-1, f"syn_op_qk_rope: positions are int32 [{T}] on the current device")
+    hq = _heads("q", q, q_out, q_gain, T, hd, dt, device) if q is not None else None
+    hk = _heads("k", k, k_out, k_gain, T, hd, dt, device) if k is not None else None
+    if T == 0:
+        return (q_out if q is not None else None), (k_out if k is not None else None)
+    code = load_library().syn_op_qk_rope(rope._h if rope is not None else None, C.addressof(hq) if hq is not None else None,
+                                         C.addressof(hk) if hk is not None else None,
+                                         positions.data_ptr() if rope is not None else None, T, hd, eps, _TYPES[dt], _TYPES[odt],
+                                         _raw_stream(stream, device))
+    if code:
+        _check(code, "syn_op_qk_rope")
+    return (q_out if q is not None else None), (k_out if k is not None else None)
+
+
 class Plan:
     """syn_plan_create / syn_verify_run / syn_op_attention / syn_plan_stats / syn_plan_free."""
 
@@ -310,6 +438,30 @@ class Plan:
             self.kv.model._h, self.kv._h, self._h, C.c_void_p(accept_len.data_ptr()), C.c_void_p(correction.data_ptr()),
             C.c_void_p(top1.data_ptr()) if top1 is not None else None,
             C.c_void_p(logits.data_ptr()) if logits is not None else None, _stream_ptr(stream)), "syn_verify_run")
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None, k_gain: Optional[torch.Tensor] = None,
+               q: Optional[torch.Tensor] = None, q_gain: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+               stream=None) -> Optional[torch.Tensor]:
+        """syn_op_kv_append: normalises (k_gain) and rotates (rope) the chunks' keys k [T, n_kv_heads, hd] and puts them, with
+        v, into the layer at the plan's slots.  With q [T, n_q_heads, hd]: returns the queries, treated the same way, as attention()
+        takes them, float16 [T, n_q_heads * hd]."""
+        s = self.kv.model.shape
+        device, T, hd = torch.cuda.current_device(), self.n_tokens, s.head_dim
+        dt = k.dtype
+        if dt not in _TYPES:
+            raise SynError(-1, "append: bfloat16, float16 or float32")
+        if q is not None and q_out is None:
+            q_out = torch.empty(T, s.q_dim, dtype=torch.float16, device=q.device)
+        if q is not None and q_out.dtype != torch.float16:
+            raise SynError(-1, "append: the queries' output is float16")
+        hq = _heads("q", q, q_out, q_gain, T, hd, dt, device) if q is not None else None
+        hk, hv = _heads("k", k, None, k_gain, T, hd, dt, device), _heads("v", v, None, None, T, hd, dt, device)
+        code = self._lib.syn_op_kv_append(self.kv.model._h, self.kv._h, self._h, layer, rope._h if rope is not None else None,
+                                          C.addressof(hq) if hq is not None else None, C.addressof(hk), C.addressof(hv), _TYPES[dt],
+                                          _raw_stream(stream, device))
+        if code:
+            _check(code, "syn_op_kv_append")
+        return q_out if q is not None else None
 
     def attention(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """syn_op_attention: q and the result are half precision [T, n_q_heads * head_dim]."""

@@ -19,6 +19,7 @@
 #include "gemm2.cuh"
 #include "gemm_thin.cuh"
 #include "pieces.h"
+#include "rope.cuh"
 #include "sampling.cuh"
 
 using namespace syn;
@@ -280,6 +281,7 @@ static int make_xmaps(XMaps* out, const void* base, uint64_t rows, uint64_t K) {
 struct syn_model {
     syn_model_desc desc;
     int f_pad, n_sm, gu_rows, qkv_rows, v_rows;
+    int device = 0;   // the weights' and workspaces' device
     bf16 *embed = nullptr, *final_norm = nullptr;
     op16* lm_head = nullptr;
     std::vector<op16*> wqkv, wo, wgu, wd;                 // projections in the packed tile layout (half precision)
@@ -543,6 +545,7 @@ static int syn_model_load_impl(const syn_model_desc* desc, const syn_weights* w,
     if (!m) return SYN_E_OOM;
     m->desc = c;
     m->n_sm = prop.multiProcessorCount;
+    m->device = dev;
     m->f_pad = (c.d_ffn + 63) / 64 * 64;
     const int d = c.d_model, q_dim = c.n_q_heads * c.head_dim, kv_dim = c.n_kv_heads * c.head_dim, f = c.d_ffn;
     m->qkv_rows = q_dim + 2 * kv_dim;
@@ -2390,6 +2393,160 @@ static int syn_op_attention_static_impl(syn_model* m, syn_kv* kv, const syn_plan
     AttnParams ap;
     attn_params(ap, m, kv, p, layer, (op16*)out, part_o, part_ml, group_count);
     return attention_kernel(m, kv, p, ap, m->tm_q, false, st) == cudaSuccess ? SYN_OK : SYN_E_CUDA;
+}
+
+// ------------------------------------------------------------------------------------------ rotation and append
+
+struct syn_rope {
+    RopeTable table;
+    double freq[ROPE_MAX_DIM / 2], amplitude;
+    int rotary_dim;
+};
+
+extern "C" int syn_rope_create(const syn_rope_desc* desc, syn_rope** out) {
+    if (!desc || !out) return SYN_E_INVALID_ARG;
+    const syn_rope_desc d = *desc;
+    const double PI = 3.14159265358979323846;
+    auto positive = [](double v) { return std::isfinite(v) && v > 0.0; };
+    if (d.rotary_dim < 2 || d.rotary_dim > ROPE_MAX_DIM || d.rotary_dim % 2 || d.layout > SYN_ROPE_INTERLEAVED || d.scaling > SYN_ROPE_SCALE_INDEX)
+        return SYN_E_INVALID_ARG;
+    if (!positive(d.base) || (d.scaling != SYN_ROPE_SCALE_NONE && !positive(d.factor))) return SYN_E_INVALID_ARG;
+    if (!(d.amplitude == 0.0 || positive(d.amplitude))) return SYN_E_INVALID_ARG;
+    if ((d.scaling == SYN_ROPE_SCALE_TURNS || d.scaling == SYN_ROPE_SCALE_INDEX) && (!positive(d.original_len) || !positive(d.low) || !std::isfinite(d.high) || d.high <= d.low))
+        return SYN_E_INVALID_ARG;
+    if (d.scaling == SYN_ROPE_SCALE_INDEX && d.base <= 1.0) return SYN_E_INVALID_ARG;
+    syn_rope* r = new (std::nothrow) syn_rope();
+    if (!r) return SYN_E_OOM;
+    const int n = (int)d.rotary_dim / 2;
+    const double dim = (double)d.rotary_dim;
+    const double base = d.scaling == SYN_ROPE_SCALE_BASE && n > 1 ? d.base * std::pow(d.factor, dim / (dim - 2.0)) : d.base;
+    double first = 0.0, last = 0.0;
+    if (d.scaling == SYN_ROPE_SCALE_INDEX) {
+        auto index_of = [&](double turns) { return dim * std::log(d.original_len / (turns * 2.0 * PI)) / (2.0 * std::log(d.base)); };
+        first = std::max(std::floor(index_of(d.high)), 0.0);
+        last = std::min(std::ceil(index_of(d.low)), dim - 1.0);
+    }
+    for (int i = 0; i < n; ++i) {
+        const double f = std::pow(base, -2.0 * i / dim);
+        double keep = 1.0;   // share of the unscaled frequency
+        if (d.scaling == SYN_ROPE_SCALE_LINEAR) keep = 0.0;
+        else if (d.scaling == SYN_ROPE_SCALE_TURNS) keep = (d.original_len * f / (2.0 * PI) - d.low) / (d.high - d.low);
+        else if (d.scaling == SYN_ROPE_SCALE_INDEX) keep = 1.0 - (i - first) / (last > first ? last - first : 0.001);
+        keep = std::min(1.0, std::max(0.0, keep));
+        r->freq[i] = keep == 1.0 ? f : f * keep + f / d.factor * (1.0 - keep);
+        r->table.turns[i] = r->freq[i] / (2.0 * PI);
+    }
+    r->amplitude = d.amplitude != 0.0 ? d.amplitude : d.scaling == SYN_ROPE_SCALE_INDEX && d.factor > 1.0 ? 0.1 * std::log(d.factor) + 1.0 : 1.0;
+    r->table.amplitude = (float)r->amplitude;
+    r->table.half = n;
+    r->table.interleaved = d.layout == SYN_ROPE_INTERLEAVED;
+    r->rotary_dim = (int)d.rotary_dim;
+    *out = r;
+    return SYN_OK;
+}
+
+extern "C" void syn_rope_free(syn_rope* r) { delete r; }
+
+extern "C" int syn_rope_freqs(const syn_rope* r, double* freqs, double* amplitude) {
+    if (!r || !freqs || !amplitude) return SYN_E_INVALID_ARG;
+    memcpy(freqs, r->freq, (size_t)r->table.half * sizeof(double));
+    *amplitude = r->amplitude;
+    return SYN_OK;
+}
+
+static int type_bytes(int type) { return type == SYN_TYPE_F32 ? 4 : 2; }
+
+// Checks one segment and takes it up; false: refused.
+static bool rope_segment(RopeParams& rp, int i, const syn_heads& h, int in_type, int out_type, int turn, int plane, bool& vec) {
+    const int64_t row = (int64_t)h.n_heads * rp.head_dim;
+    if (!h.x || h.n_heads < 1 || h.n_heads > 65536 || h.x_stride < row) return false;
+    if (((uintptr_t)h.x % type_bytes(in_type)) || ((uintptr_t)h.gain & 1)) return false;
+    if (plane < 0) {
+        if (!h.y || h.y_stride < row || (uintptr_t)h.y % type_bytes(out_type)) return false;
+        if (h.y == h.x && (h.y_stride != h.x_stride || type_bytes(in_type) != type_bytes(out_type))) return false;
+        vec = vec && (((uintptr_t)h.y | (uintptr_t)(h.y_stride * type_bytes(out_type))) & 15) == 0;
+    } else if (h.y) return false;
+    vec = vec && (((uintptr_t)h.x | (uintptr_t)(h.x_stride * type_bytes(in_type))) & 15) == 0;
+    rp.seg[i] = RopeSeg{h.x, h.x_stride, h.y, h.y_stride, (const bf16*)h.gain, rp.n_heads += h.n_heads, turn, plane};
+    return true;
+}
+
+template <typename TIN, typename TOUT, bool VEC, int NV>
+static int rope_launch_nv(const RopeParams& rp, int threads, cudaStream_t st) {
+    const dim3 grid((unsigned)((rp.T + NV - 1) / NV), (unsigned)((rp.n_heads + rp.heads_per_block - 1) / rp.heads_per_block));
+    rope_kernel<TIN, TOUT, VEC, NV><<<grid, threads, 0, st>>>(rp);
+    return launch_ok() ? SYN_OK : SYN_E_CUDA;
+}
+template <typename TIN, typename TOUT>
+static int rope_launch_types(const RopeParams& rp, int threads, bool vec, cudaStream_t st) {
+    return vec ? rope_launch_nv<TIN, TOUT, true, 1>(rp, threads, st) : rope_launch_nv<TIN, TOUT, false, 1>(rp, threads, st);
+}
+static int rope_launch(RopeParams& rp, int in_type, int out_type, bool vec, cudaStream_t st) {
+    int lanes = 1;   // of a head
+    while (lanes * 8 < rp.head_dim) lanes *= 2;
+    // as few blocks per token as hold all heads, filled evenly; whole warps
+    const int unit = std::max(1, 32 / lanes), most = ROPE_THREADS / lanes;
+    const int blocks = (rp.n_heads + most - 1) / most;
+    rp.heads_per_block = ((rp.n_heads + blocks - 1) / blocks + unit - 1) / unit * unit;
+    const int threads = rp.heads_per_block * lanes;
+    if (in_type == SYN_TYPE_BF16)
+        return out_type == in_type ? rope_launch_types<bf16, bf16>(rp, threads, vec, st) : rope_launch_types<bf16, op16>(rp, threads, vec, st);
+    if (in_type == SYN_TYPE_F16) return rope_launch_types<op16, op16>(rp, threads, vec, st);
+    return out_type == in_type ? rope_launch_types<float, float>(rp, threads, vec, st) : rope_launch_types<float, op16>(rp, threads, vec, st);
+}
+
+static bool rope_types_ok(int in_type, int out_type) {
+    return in_type >= SYN_TYPE_BF16 && in_type <= SYN_TYPE_F32 && (out_type == in_type || out_type == SYN_TYPE_F16);
+}
+
+extern "C" int syn_op_qk_rope(const syn_rope* rope, const syn_heads* q, const syn_heads* k, const int32_t* positions, int32_t T, int32_t head_dim,
+                              float eps, int32_t in_type, int32_t out_type, void* cuda_stream) {
+    if ((!q && !k) || T < 0 || head_dim < 8 || head_dim > ROPE_MAX_DIM || head_dim % 8 || !(eps >= 0.f) || !rope_types_ok(in_type, out_type))
+        return SYN_E_INVALID_ARG;
+    if (rope && (!positions || rope->rotary_dim > head_dim)) return SYN_E_INVALID_ARG;
+    RopeParams rp;
+    memset(&rp, 0, sizeof(rp));
+    if (rope) rp.rope = rope->table;
+    rp.pos = positions;
+    rp.T = T; rp.head_dim = head_dim; rp.eps = eps;
+    bool vec = true;
+    int n = 0;
+    for (const syn_heads* h : {q, k})
+        if (h && !rope_segment(rp, n++, *h, in_type, out_type, 1, -1, vec)) return SYN_E_INVALID_ARG;
+    for (; n < 3; ++n) rp.seg[n].end = rp.n_heads;
+    if (T == 0) return SYN_OK;
+    return rope_launch(rp, in_type, out_type, vec, reinterpret_cast<cudaStream_t>(cuda_stream));
+}
+
+extern "C" int syn_op_kv_append(syn_model* m, syn_kv* kv, const syn_plan* p, uint32_t layer, const syn_rope* rope, const syn_heads* q,
+                                const syn_heads* k, const syn_heads* v, int32_t in_type, void* cuda_stream) {
+    if (!m || !kv || !p || kv->model != m || !plan_matches(p, kv) || layer >= m->desc.n_layers || !k || !v || !rope_types_ok(in_type, SYN_TYPE_F16))
+        return SYN_E_INVALID_ARG;
+    const syn_model_desc& c = m->desc;
+    int dev = -1;
+    CU_OK(cudaGetDevice(&dev));
+    if (dev != m->device || (rope && rope->rotary_dim > (int)c.head_dim)) return SYN_E_INVALID_ARG;
+    if ((q && q->n_heads != (int)c.n_q_heads) || k->n_heads != (int)c.n_kv_heads || v->n_heads != (int)c.n_kv_heads || v->gain)
+        return SYN_E_INVALID_ARG;
+    RopeParams rp;
+    memset(&rp, 0, sizeof(rp));
+    if (rope) rp.rope = rope->table;
+    rp.pos = p->d<int>(p->o_pos);
+    rp.slot = p->d<int>(p->o_slot);
+    rp.pool = kv->pool + kv->layer_elems * layer;
+    rp.T = p->T; rp.head_dim = c.head_dim; rp.n_kv_heads = c.n_kv_heads; rp.eps = c.rms_eps;
+    bool vec = true;
+    if (q && !rope_segment(rp, 0, *q, in_type, SYN_TYPE_F16, 1, -1, vec)) return SYN_E_INVALID_ARG;
+    if (!rope_segment(rp, 1, *k, in_type, SYN_TYPE_F16, 1, 0, vec) || !rope_segment(rp, 2, *v, in_type, SYN_TYPE_F16, 0, 1, vec))
+        return SYN_E_INVALID_ARG;
+    return rope_launch(rp, in_type, SYN_TYPE_F16, vec, reinterpret_cast<cudaStream_t>(cuda_stream));
+}
+
+extern "C" int syn_kv_layer(const syn_kv* kv, uint32_t layer, void** pool, int64_t* n_elements) {
+    if (!kv || !pool || !n_elements || layer >= kv->model->desc.n_layers) return SYN_E_INVALID_ARG;
+    *pool = kv->pool + kv->layer_elems * layer;
+    *n_elements = (int64_t)kv->layer_elems;
+    return SYN_OK;
 }
 
 // The projection schedule without a device (tests): the launch shape, and work item i of CTA `cta`.
