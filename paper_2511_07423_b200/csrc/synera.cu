@@ -2456,43 +2456,64 @@ extern "C" int syn_rope_freqs(const syn_rope* r, double* freqs, double* amplitud
 
 static int type_bytes(int type) { return type == SYN_TYPE_F32 ? 4 : 2; }
 
+constexpr int ROPE_MAX_HEADS = 16384;   // of a segment: chunks of one head are the grid's second dimension
+
 // Checks one segment and takes it up; false: refused.
 static bool rope_segment(RopeParams& rp, int i, const syn_heads& h, int in_type, int out_type, int turn, int plane, bool& vec) {
     const int64_t row = (int64_t)h.n_heads * rp.head_dim;
-    if (!h.x || h.n_heads < 1 || h.n_heads > 65536 || h.x_stride < row) return false;
+    if (!h.x || h.n_heads < 1 || h.n_heads > ROPE_MAX_HEADS || h.x_stride < row) return false;
     if (((uintptr_t)h.x % type_bytes(in_type)) || ((uintptr_t)h.gain & 1)) return false;
     if (plane < 0) {
         if (!h.y || h.y_stride < row || (uintptr_t)h.y % type_bytes(out_type)) return false;
         if (h.y == h.x && (h.y_stride != h.x_stride || type_bytes(in_type) != type_bytes(out_type))) return false;
         vec = vec && (((uintptr_t)h.y | (uintptr_t)(h.y_stride * type_bytes(out_type))) & 15) == 0;
     } else if (h.y) return false;
-    vec = vec && (((uintptr_t)h.x | (uintptr_t)(h.x_stride * type_bytes(in_type))) & 15) == 0;
-    rp.seg[i] = RopeSeg{h.x, h.x_stride, h.y, h.y_stride, (const bf16*)h.gain, rp.n_heads += h.n_heads, turn, plane};
+    vec = vec && (((uintptr_t)h.x | (uintptr_t)(h.x_stride * type_bytes(in_type))) & 15) == 0 && ((uintptr_t)h.gain & 15) == 0;
+    rp.seg[i] = RopeSeg{h.x, h.x_stride, h.y, h.y_stride, (const bf16*)h.gain, h.n_heads, 0, turn, plane};
     return true;
 }
 
-template <typename TIN, typename TOUT, bool VEC, int NV>
-static int rope_launch_nv(const RopeParams& rp, int threads, cudaStream_t st) {
-    const dim3 grid((unsigned)((rp.T + NV - 1) / NV), (unsigned)((rp.n_heads + rp.heads_per_block - 1) / rp.heads_per_block));
-    rope_kernel<TIN, TOUT, VEC, NV><<<grid, threads, 0, st>>>(rp);
+struct RopeLaunch {
+    dim3 grid;
+    int threads, mode, unroll;
+};
+template <typename TIN, typename TOUT, int MODE>
+static int rope_launch_mode(const RopeParams& rp, const RopeLaunch& la, cudaStream_t st) {
+    if (la.unroll == 1) rope_kernel<TIN, TOUT, MODE, 1><<<la.grid, la.threads, 0, st>>>(rp);
+    else rope_kernel<TIN, TOUT, MODE, ROPE_UNROLL><<<la.grid, la.threads, 0, st>>>(rp);
     return launch_ok() ? SYN_OK : SYN_E_CUDA;
 }
 template <typename TIN, typename TOUT>
-static int rope_launch_types(const RopeParams& rp, int threads, bool vec, cudaStream_t st) {
-    return vec ? rope_launch_nv<TIN, TOUT, true, 1>(rp, threads, st) : rope_launch_nv<TIN, TOUT, false, 1>(rp, threads, st);
+static int rope_launch_types(const RopeParams& rp, const RopeLaunch& la, cudaStream_t st) {
+    switch (la.mode) {
+        case ROPE_SCALAR: return rope_launch_mode<TIN, TOUT, ROPE_SCALAR>(rp, la, st);
+        case ROPE_VEC_PAIRS: return rope_launch_mode<TIN, TOUT, ROPE_VEC_PAIRS>(rp, la, st);
+        default: return rope_launch_mode<TIN, TOUT, ROPE_VEC_HALVES>(rp, la, st);
+    }
 }
+// Heads of a warp.  All of a token's share its angles (two cosines and sines a lane), so a warp takes up to 5 rounds of
+// ROPE_UNROLL accesses while 16 warps to an SM remain; below 20 accesses to an SM one each, for the latency.  Measured, 8B heads,
+// bf16, us: 8192 tokens with one access in flight 39, four 34; 512 tokens with one access a warp 9.9, four 5.4; 64 tokens 3.6 and 4.0.
+constexpr int ROPE_SM_ACCESSES = 20, ROPE_SM_WARPS = 16, ROPE_MAX_ROUNDS = 5;
 static int rope_launch(RopeParams& rp, int in_type, int out_type, bool vec, cudaStream_t st) {
-    int lanes = 1;   // of a head
-    while (lanes * 8 < rp.head_dim) lanes *= 2;
-    // as few blocks per token as hold all heads, filled evenly; whole warps
-    const int unit = std::max(1, 32 / lanes), most = ROPE_THREADS / lanes;
-    const int blocks = (rp.n_heads + most - 1) / most;
-    rp.heads_per_block = ((rp.n_heads + blocks - 1) / blocks + unit - 1) / unit * unit;
-    const int threads = rp.heads_per_block * lanes;
-    if (in_type == SYN_TYPE_BF16)
-        return out_type == in_type ? rope_launch_types<bf16, bf16>(rp, threads, vec, st) : rope_launch_types<bf16, op16>(rp, threads, vec, st);
-    if (in_type == SYN_TYPE_F16) return rope_launch_types<op16, op16>(rp, threads, vec, st);
-    return out_type == in_type ? rope_launch_types<float, float>(rp, threads, vec, st) : rope_launch_types<float, op16>(rp, threads, vec, st);
+    while ((8 << rp.lane_bits) < rp.head_dim) ++rp.lane_bits;
+    rp.inv_hd = 1.0f / (float)rp.head_dim;
+    const int per = 32 >> rp.lane_bits;
+    int64_t units = 0;   // accesses of a warp
+    for (const RopeSeg& s : rp.seg) units += (int64_t)rp.T * ((s.n_heads + per - 1) / per);
+    RopeLaunch la;
+    la.unroll = units < 148 * ROPE_SM_ACCESSES ? 1 : ROPE_UNROLL;
+    const int64_t rounds = units / (148 * ROPE_SM_WARPS * ROPE_UNROLL);   // (0 where unroll is 1)
+    rp.heads_per_warp = per * la.unroll * (int)std::min<int64_t>(std::max<int64_t>(rounds, 1), ROPE_MAX_ROUNDS);
+    int chunks = 0;
+    for (RopeSeg& s : rp.seg) s.end = chunks += (s.n_heads + rp.heads_per_warp - 1) / rp.heads_per_warp;
+    const int warps = std::min(ROPE_WARPS, rp.T);
+    la.grid = dim3((unsigned)((rp.T + warps - 1) / warps), (unsigned)chunks);
+    la.threads = 32 * warps;
+    la.mode = !vec || (!rp.rope.interleaved && rp.rope.half % 4) ? ROPE_SCALAR : rp.rope.interleaved ? ROPE_VEC_PAIRS : ROPE_VEC_HALVES;
+    if (in_type == SYN_TYPE_BF16) return out_type == in_type ? rope_launch_types<bf16, bf16>(rp, la, st) : rope_launch_types<bf16, op16>(rp, la, st);
+    if (in_type == SYN_TYPE_F16) return rope_launch_types<op16, op16>(rp, la, st);
+    return out_type == in_type ? rope_launch_types<float, float>(rp, la, st) : rope_launch_types<float, op16>(rp, la, st);
 }
 
 static bool rope_types_ok(int in_type, int out_type) {
@@ -2513,7 +2534,6 @@ extern "C" int syn_op_qk_rope(const syn_rope* rope, const syn_heads* q, const sy
     int n = 0;
     for (const syn_heads* h : {q, k})
         if (h && !rope_segment(rp, n++, *h, in_type, out_type, 1, -1, vec)) return SYN_E_INVALID_ARG;
-    for (; n < 3; ++n) rp.seg[n].end = rp.n_heads;
     if (T == 0) return SYN_OK;
     return rope_launch(rp, in_type, out_type, vec, reinterpret_cast<cudaStream_t>(cuda_stream));
 }
