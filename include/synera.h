@@ -172,6 +172,20 @@ int syn_plan_create(syn_model *m, syn_kv *kv, int32_t n_req, const int32_t *chun
                     const int32_t *chunk_offsets, const int32_t *page_tables, int32_t max_pages,
                     const int32_t *ctx_lens, const int32_t *n_uncached, syn_plan **out);
 void syn_plan_free(syn_plan *p);
+
+/* A plan for a batch whose requests share prefixes (one system prompt for all devices, a document for some), whose attention
+ * meets the shared keys once for all requests that share them instead of once a request.  Arguments, validation and errors are
+ * syn_plan_create's, and so is what the plan is good for (syn_verify_run, syn_op_attention, syn_op_kv_append, ...).  What is shared is read off
+ * the page tables: requests next to each other in the batch whose rows begin with the same pages share those that are full
+ * and cached for each of them (page i where (i + 1) * page_size <= ctx_lens), from 128 keys on; runs of neighbours that have more
+ * in common than the run around them form further levels.  So put requests that share next to each other.  The
+ * batch is planned as by syn_plan_create where nothing is shared or the planner expects no gain; syn_plan_attention tells
+ * (4: shared).  A shared plan holds the fp32 partial results of its own attention (calls on one plan must not overlap), so
+ * syn_op_attention and syn_op_attention_static allocate nothing and copy nothing with it: q there is read in place and must be
+ * aligned to 16 bytes, out to 8 (SYN_E_INVALID_ARG).  Values of K and V behind a request's last token do not reach its result, whatever they are. */
+int syn_plan_create_shared(syn_model *m, syn_kv *kv, int32_t n_req, const int32_t *chunk_tokens,
+                           const int32_t *chunk_offsets, const int32_t *page_tables, int32_t max_pages,
+                           const int32_t *ctx_lens, const int32_t *n_uncached, syn_plan **out);
 int syn_verify_run(syn_model *m, syn_kv *kv, const syn_plan *p, int32_t *accept_len_dev,
                    int32_t *correction_dev, int32_t *top1_dev, float *logits_out, void *cuda_stream);
 int syn_model_status(syn_model *m); /* SYN_OK or SYN_E_DEVICE_TIMEOUT / SYN_E_CUDA; blocking */
@@ -181,12 +195,12 @@ typedef struct {
     int32_t n_req, n_tokens;       /* B and T                                               */
     int64_t ctx_tokens;            /* sum of ctx_lens                                       */
     int64_t weight_bytes;          /* bf16 bytes of all projections streamed once per step  */
-    int64_t kv_read_bytes;         /* sum over requests of (ctx+n) * 2*Hkv*hd*2 * n_layers   */
+    int64_t kv_read_bytes;         /* sum over requests of (ctx+n) * 2*Hkv*hd*2 * n_layers; keys that are met once for several requests count once */
     int64_t kv_write_bytes;        /* T * 2*Hkv*hd*2 * n_layers                             */
     double dense_flops;            /* 2 * rows * parameters of every projection: T rows, in the lm_head of a step without logits and argmaxes perhaps fewer (syn_verify_run) */
     double attn_flops;             /* 4 * Hq*hd * n_layers * sum over tokens of keys seen    */
     int32_t attn_items, attn_split_items; /* attention work items per layer / those that are partial */
-    int32_t kernel_launches;       /* kernels launched by one syn_verify_run: 1 + 5 n_layers + 2, one more where the lm_head runs over fewer rows */
+    int32_t kernel_launches;       /* kernels launched by one syn_verify_run: 1 + 5 n_layers + 2, one more where the lm_head runs over fewer rows, one more a layer with shared prefixes (the merge) */
     int32_t attn_rows;             /* row tile of the attention kernel the batch was planned for: 64 (warp-level MMAs) or 128 (tcgen05); the kernel: syn_plan_attention */
     int64_t h2d_bytes;             /* batch description uploaded per step by syn_verify_batch */
     double t_gpu_ms;               /* device time of the step, first kernel to last (CUDA events); 0 unless profiling is on */
@@ -199,8 +213,8 @@ typedef struct {
  * logits or argmaxes asked for. */
 int syn_last_step_stats(syn_model *m, syn_step_stats *out);
 int syn_plan_stats(const syn_plan *p, syn_step_stats *out);
-/* The attention kernel a plan was laid out for, numbered as in syn_debug_set_attention: 1, 2 or 3 (attn_rows is 64 for 1
- * and 3).  Which kernel a projection takes: syn_thin_plan_host, then syn_gemm2_plan_host.  Errors: SYN_E_INVALID_ARG. */
+/* The attention kernel a plan was laid out for, numbered as in syn_debug_set_attention: 1, 2, 3 or, for plans of
+ * syn_plan_create_shared, 4 (attn_rows is 64 for 1 and 3, 128 for 2 and 4).  Which kernel a projection takes: syn_thin_plan_host, then syn_gemm2_plan_host.  Errors: SYN_E_INVALID_ARG. */
 int syn_plan_attention(const syn_plan *p);
 
 /* The host planner of syn_plan_create / syn_verify_batch on its own, without a device: the same
@@ -233,6 +247,19 @@ int syn_plan_work_host(const syn_model_desc *desc, uint32_t n_pages, uint32_t pa
                        int32_t items_cap, int32_t *n_items, int32_t *cta_begin, int32_t *n_cta, int32_t *attention,
                        syn_step_stats *stats);
 
+/* The work list of syn_plan_create_shared on n_sm SMs (at most 32767), whether or not the planner would take it (*taken); arguments and
+ * validation as in syn_plan_host.  items [items_cap][SYN_SHARED_ITEM_FIELDS], in CTA order: (first query token, query tokens,
+ * kv head, request whose page table is read, first key, one past the last key, position of the first query token or -1 where
+ * every token sees every key, first row of its partial results, tiles of rows 1 or 2).  parts [parts_cap][3]: (token, kv head, row), sorted by the first
+ * two: the rows of partial results that are merged for the kv head's first query head; an item of one tile and more than one stage of 128 keys
+ * leaves two, of its even and its odd stages.  SYN_E_CAPACITY if a capacity is too small, *n_items and *n_parts then hold the counts needed; NULL to
+ * skip an array.  stats may be NULL. */
+#define SYN_SHARED_ITEM_FIELDS 9
+int syn_plan_shared_host(const syn_model_desc *desc, uint32_t n_pages, uint32_t page_size, int32_t n_sm, int32_t n_req,
+                         const int32_t *chunk_tokens, const int32_t *chunk_offsets, const int32_t *page_tables,
+                         int32_t max_pages, const int32_t *ctx_lens, const int32_t *n_uncached, int32_t *items,
+                         int32_t items_cap, int32_t *n_items, int32_t *cta_begin, int32_t *n_cta, int32_t *parts,
+                         int32_t parts_cap, int32_t *n_parts, int32_t *taken, syn_step_stats *stats);
 
 /* Per-kernel-class device timing.  With profiling on, syn_verify_run / syn_verify_batch bracket
  * every launch with CUDA events on the caller's stream.  syn_get_profile synchronises the device,
@@ -283,7 +310,8 @@ int syn_op_linear_reset(void);
  * keeps its kernel): 0 (default) the cheapest for the batch by the planner's cost model, 1 the
  * warp-level-MMA kernel (row tiles of 64), 2 the tcgen05 kernel (row tiles of 128: a whole chunk of up to
  * 128 / G tokens is one work item per kv head), 3 the warp-level-MMA kernel in CTAs of half an SM (row tiles of
- * 64; few requests).  Process-wide. */
+ * 64; few requests); with 1 to 3 plans of syn_plan_create_shared take that kernel too, with 4 they take the one for
+ * shared prefixes whatever the estimates, and other plans are as with 0.  Process-wide. */
 int syn_debug_set_spin_limit(int64_t cycles);
 int syn_debug_linear_counter(int32_t index, int32_t value);
 int syn_debug_set_schedule(int32_t which);

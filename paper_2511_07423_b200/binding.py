@@ -63,7 +63,8 @@ EXPORTS = ["syn_model_load", "syn_model_free", "syn_kv_alloc", "syn_kv_free", "s
            "syn_op_attention", "syn_op_attention_static",
            "syn_set_profile", "syn_get_profile", "syn_verify_batch_sampled", "syn_op_sample_verify",
            "syn_gemm_plan_host", "syn_gemm_work_host", "syn_gemm2_plan_host", "syn_gemm2_work_host",
-           "syn_thin_plan_host", "syn_rope_create", "syn_rope_free", "syn_rope_freqs", "syn_op_qk_rope", "syn_op_kv_append", "syn_kv_layer"]
+           "syn_thin_plan_host", "syn_rope_create", "syn_rope_free", "syn_rope_freqs", "syn_op_qk_rope", "syn_op_kv_append", "syn_kv_layer", "syn_plan_create_shared",
+           "syn_plan_shared_host"]
 SCHED_EXPORTS = ["syn_sched_create", "syn_sched_free", "syn_sched_add_request", "syn_sched_add_verify", "syn_sched_finish",
                  "syn_sched_peek", "syn_sched_commit", "syn_sched_step", "syn_sched_get_stats"]
 
@@ -411,19 +412,20 @@ def syn_op_qk_rope(rope: Optional[Rope], q: Optional[torch.Tensor], k: Optional[
 
 
 class Plan:
-    """syn_plan_create / syn_verify_run / syn_op_attention / syn_plan_stats / syn_plan_free."""
+    """syn_plan_create, or with share_prefix syn_plan_create_shared / syn_verify_run / syn_op_attention / syn_plan_stats / syn_plan_free."""
 
-    def __init__(self, kv: KVCache, chunk_tokens, chunk_offsets, page_tables, ctx_lens, n_uncached=None):
+    def __init__(self, kv: KVCache, chunk_tokens, chunk_offsets, page_tables, ctx_lens, n_uncached=None, share_prefix: bool = False):
         self._lib = load_library()
         self.kv = kv
         tok, off, ctx, pt = _i32(chunk_tokens), _i32(chunk_offsets), _i32(ctx_lens), _i32(page_tables)
         unc = _i32(n_uncached) if n_uncached is not None else None
         self.n_req, self.n_tokens = ctx.numel(), int(off[-1])
         self._h = C.c_void_p()
-        _check(self._lib.syn_plan_create(
+        create = self._lib.syn_plan_create_shared if share_prefix else self._lib.syn_plan_create
+        _check(create(
             kv.model._h, kv._h, C.c_int32(self.n_req), C.c_void_p(tok.data_ptr()), C.c_void_p(off.data_ptr()),
             C.c_void_p(pt.data_ptr()), C.c_int32(pt.shape[1]), C.c_void_p(ctx.data_ptr()),
-            C.c_void_p(unc.data_ptr()) if unc is not None else None, C.byref(self._h)), "syn_plan_create")
+            C.c_void_p(unc.data_ptr()) if unc is not None else None, C.byref(self._h)), "syn_plan_create_shared" if share_prefix else "syn_plan_create")
 
     def stats(self) -> StepStats:
         s = StepStats()
@@ -567,6 +569,30 @@ def plan_work_host(shape, n_pages: int, chunk_tokens, chunk_offsets, page_tables
         if items is None:
             items = torch.zeros(n_items.value, len(WORK_ITEM_FIELDS), dtype=torch.int32)
     return {"items": items, "cta_begin": cta[:n_cta.value + 1], "n_cta": n_cta.value, "attention": kind.value, "stats": st}
+
+
+SHARED_ITEM_FIELDS = ("q_tok", "n_tok", "kvh", "req", "kv_begin", "kv_end", "q_pos0", "base", "tiles")
+
+
+def plan_shared_host(shape, n_pages: int, chunk_tokens, chunk_offsets, page_tables, ctx_lens, n_uncached=None,
+                     n_sm: int = 148, page_size: int = 16):
+    """syn_plan_shared_host: the work list of a plan that shares prefixes.  Returns a dict with items [n_items, 9] (columns
+    SHARED_ITEM_FIELDS), cta_begin [n_cta + 1], n_cta, parts [n_parts, 3] (token, kv head, row), taken and stats."""
+    lib = load_library()
+    args, _keep, _ = _host_plan_args(shape, n_pages, n_sm, page_size, chunk_tokens, chunk_offsets, page_tables, ctx_lens, n_uncached)
+    cta = torch.zeros(max(n_sm, 0) + 1, dtype=torch.int32)
+    n_items, n_cta, n_parts, taken = C.c_int32(0), C.c_int32(0), C.c_int32(0), C.c_int32(0)
+    st = StepStats()
+    items = parts = None
+    for _ in range(2):
+        code = lib.syn_plan_shared_host(*args, C.c_void_p(items.data_ptr()) if items is not None else None, n_items, C.byref(n_items),
+                                        C.c_void_p(cta.data_ptr()), C.byref(n_cta), C.c_void_p(parts.data_ptr()) if parts is not None else None,
+                                        n_parts, C.byref(n_parts), C.byref(taken), C.byref(st))
+        _check(code, "syn_plan_shared_host")
+        if items is None:
+            items = torch.zeros(n_items.value, len(SHARED_ITEM_FIELDS), dtype=torch.int32)
+            parts = torch.zeros(n_parts.value, 3, dtype=torch.int32)
+    return {"items": items, "cta_begin": cta[:n_cta.value + 1], "n_cta": n_cta.value, "parts": parts, "taken": bool(taken.value), "stats": st}
 
 
 # ------------------------------------------------------------------------------------------ scheduler
@@ -778,7 +804,7 @@ def debug_set_schedule(which: int) -> None:
 
 
 def debug_set_attention(which: int) -> None:
-    """syn_debug_set_attention: 0 default, 1 warp-level-MMA kernel, 2 tcgen05 kernel, 3 half-SM kernel; applies to plans made afterwards."""
+    """syn_debug_set_attention: 0 default, 1 warp-level-MMA kernel, 2 tcgen05 kernel, 3 half-SM kernel; 4 plans with share_prefix take the shared-prefix kernel in any case; applies to plans made afterwards."""
     _check(load_library().syn_debug_set_attention(C.c_int32(which)), "syn_debug_set_attention")
 
 

@@ -1,0 +1,514 @@
+// Attention of a batch whose requests share prefixes: the tokens of all requests that share a run of keys meet them
+// together, once, on the tensor-memory path (shared_plan.h cuts the work; the formula is attention.cuh's).
+//
+// An item is some query tokens (of one request or of many), a kv head and a range of keys.  Its rows (row = j * G + g) are one
+// or two tiles of 128; every item leaves fp32 partials (m, l, O) per row, which shared_merge_kernel joins:
+//   out = sum_k 2^(m_k - m) O_k / sum_k 2^(m_k - m) l_k,  m = max_k m_k.
+// Both products run on tcgen05.mma with M = 128, in stages of 128 keys (8 pages):
+//   S = Q K^T : A = a Q tile, B = the stage's K, D = S in tensor memory (128 columns a tile);
+//   O += P V  : A = P in half precision in tensor memory, over the first 64 columns of S, B = V as it lies in the cache, D = O.
+// P in tensor memory leaves shared memory's bandwidth to the operands: with both of a product's operands there, a k-step of 64
+// cycles reads 8 KB, all that 128 bytes a cycle can deliver.
+// Two groups of four softmax warps (thread = row), each with its own S, P and O.  With two tiles a group owns a tile and takes
+// every stage: one read of K and V from L2 serves 256 rows, and while one group computes its exponentials the tensor
+// cores work for the other.  With one tile the groups take alternate stages, as in attention2.cuh, and leave separate partials.
+// What bounds it: with two tiles the exponentials (16 a cycle and SM, as many cycles as the products take at full rate) and the
+// products in turn; with one tile the keys' bytes.
+// Warp roles: warp 3 streams pages and Q tiles (K and V have rings of their own), one thread of warp 2 issues every MMA, warps 4..7
+// and 8..11 are the softmax groups.  tcgen05 operations of one thread complete in order, so Q K^T of a group's next stage may
+// follow P V of its last in the same columns, and the commit behind it tells that both are done.  The maximum that P is relative to
+// is raised only when a stage exceeds it by 2^8; P is scaled by 2^7 besides (at most 2^15 in half precision, so that weights down to
+// 2^-21 of the largest keep all their bits).  Every wait is bounded.
+#pragma once
+#include "attention2.cuh"
+#include "shared_plan.h"
+
+namespace syn {
+
+constexpr int SHR_THREADS = 384;
+constexpr int SHR_PAGES = SHARED_STAGE / 16;
+constexpr int SHR_SOFTMAX_REGS = 208, SHR_OTHER_REGS = 88;
+static_assert(8 * SHR_SOFTMAX_REGS + 4 * SHR_OTHER_REGS <= 12 * ATT_LAUNCH_REGS, "the increase must fit in what the others give back");
+constexpr int SHR_PRODUCER_WARP = 3, SHR_MMA_WARP = 2;
+constexpr float SHR_P_SCALE_LOG2 = 7.0f;
+
+struct SharedParams {
+    const SharedItem* items;     // by CTA
+    const int* cta_begin;        // [n_cta + 1]
+    const int* page_tables;      // [B][max_pages]
+    int max_pages, n_kv_heads, group, q_dim;
+    int tile_tokens;             // tokens of a tile: 128 / G
+    int layer_block0;            // 2 * layer * n_pages * Hkv: first (K|V) block of this layer in the pool map
+    float scale_log2;            // log2(e) / sqrt(hd)
+    float* part_o;               // [n_rows][hd]
+    float2* part_ml;             // [n_rows] (reference exponent, sum)
+    int* status;                 // 0 ok, 1 a bounded wait ran out, 2 the work list failed a bounds check
+    const int *seg_of_token, *seg_first, *list_begin, *list;   // SharedPlan's
+    op16* out;                   // [T][q_dim]
+    int n_items, n_req, n_tokens, n_pages, n_rows, n_list, n_seg;
+};
+
+// The work list is host-made; the kernel still refuses an item that would index out of bounds.
+__device__ __forceinline__ bool shared_item_ok(const SharedItem& it, const SharedParams& p) {
+    const int stages = (it.kv_end - it.kv_begin + SHARED_STAGE - 1) / SHARED_STAGE;
+    const int64_t rows = (int64_t)it.n_tok * p.group * (it.tiles == 1 && stages > 1 ? 2 : 1);
+    return it.q_tok >= 0 && it.n_tok >= 1 && it.q_tok + it.n_tok <= p.n_tokens && (it.tiles == 1 || it.tiles == 2) && it.n_tok <= it.tiles * p.tile_tokens &&
+           it.kvh >= 0 && it.kvh < p.n_kv_heads && it.req >= 0 && it.req < p.n_req && it.kv_begin >= 0 && (it.kv_begin & 15) == 0 &&
+           it.kv_begin < it.kv_end && ((it.kv_end - 1) >> 4) < p.max_pages && it.base >= 0 && it.base + rows <= p.n_rows;
+}
+
+template <int HD>
+struct SharedSmem {
+    static constexpr int HALVES = HD / 64;
+    static constexpr int GROUP_BYTES = HALVES * 1024;                 // 8 keys: [64-dim half][8 rows][128 bytes]
+    static constexpr int BOX_BYTES = 2 * GROUP_BYTES;                 // the K rows (or the V rows) of a page
+    static constexpr int K_BYTES = SHR_PAGES * BOX_BYTES;             // K (or V) of a stage
+    static constexpr int Q_HALF = 128 * 128, Q_BYTES = HALVES * Q_HALF;   // a tile: [half][128 rows][128 bytes]
+    static constexpr int K_SLOTS = HD == 128 ? 2 : 5, V_SLOTS = HD == 128 ? 3 : 6;
+    static constexpr int TOTAL = 1024 + 2 * Q_BYTES + (K_SLOTS + V_SLOTS) * K_BYTES + 512;
+    static_assert(TOTAL <= 232448, "shared memory of one CTA");
+    static constexpr int TMEM_COLS = 512;   // O of the two groups at 0 and 128; S (and P) at 256 and 384
+};
+
+// D[tmem] (+)= A[tmem] * B[smem]; one thread issues.
+__device__ __forceinline__ void umma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+template <int HD>
+__global__ void __launch_bounds__(SHR_THREADS, 1)
+attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmKV, SharedParams p) {
+    using SM = SharedSmem<HD>;
+    constexpr int HALVES = SM::HALVES, KS = SM::K_SLOTS, VS = SM::V_SLOTS;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* qbuf = smem;                               // two slots
+    uint8_t* kring = qbuf + 2 * SM::Q_BYTES;
+    uint8_t* vring = kring + KS * SM::K_BYTES;
+    uint64_t* k_full = reinterpret_cast<uint64_t*>(vring + VS * SM::K_BYTES);
+    uint64_t* k_empty = k_full + KS;     // every score of the stage is complete
+    uint64_t* v_full = k_empty + KS;
+    uint64_t* v_empty = v_full + VS;     // every P V of the stage is complete
+    uint64_t* q_full = v_empty + VS;     // [slot]
+    uint64_t* q_empty = q_full + 2;      // [slot] the last Q K^T that reads it is complete
+    uint64_t* s_full = q_empty + 2;      // [group] scores of a stage (and every P V before) are complete
+    uint64_t* p_full = s_full + 2;       // [group] P of a stage is in tensor memory (and O rescaled if need be)
+    uint64_t* o_full = p_full + 2;       // [group] the item's last P V is complete
+    uint64_t* o_empty = o_full + 2;      // [group] its warps have read O
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_empty + 2);
+    static_assert((2 * KS + 2 * VS + 12) * 8 + 4 <= 512, "barrier area");
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int it_begin = p.cta_begin[blockIdx.x], it_end = p.cta_begin[blockIdx.x + 1];
+    const int G = p.group;
+    const bool list_ok = it_begin >= 0 && it_begin <= it_end && it_end <= p.n_items;
+
+    if (threadIdx.x == 0) {
+        tma_prefetch_desc(&tmQ);
+        tma_prefetch_desc(&tmKV);
+        for (int s = 0; s < KS; ++s) { mbar_init(&k_full[s], 1); mbar_init(&k_empty[s], 1); }
+        for (int s = 0; s < VS; ++s) { mbar_init(&v_full[s], 1); mbar_init(&v_empty[s], 1); }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&q_full[s], 1);
+            mbar_init(&q_empty[s], 1);
+            mbar_init(&s_full[s], 1);
+            mbar_init(&p_full[s], 4);
+            mbar_init(&o_full[s], 1);
+            mbar_init(&o_empty[s], 4);
+        }
+        mbar_fence_init();
+        if (!list_ok) atomicExch(p.status, 2);
+    }
+    if (warp == SHR_MMA_WARP) {
+        tmem_alloc(tmem_slot, SM::TMEM_COLS);
+        tmem_relinquish();
+    }
+    pdl_launch_dependents();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    pdl_wait();   // Q and the chunk's K/V come from the preceding kernel
+
+    if (warp < 4) {
+        reg_dealloc<SHR_OTHER_REGS>();
+        if (warp == SHR_PRODUCER_WARP) {
+            // -------------------------------------------------------- producer: lanes 0..7 request a page each
+            uint32_t st = 0, qs = 0;   // stages, Q slots so far
+            bool ok = true;
+            for (int it = it_begin; list_ok && it < it_end && ok; ++it) {
+                const SharedItem item = p.items[it];
+                if (!shared_item_ok(item, p)) break;   // the other roles flag it and stop as well
+                if (lane == 0) {
+                    for (int w = 0; w < item.tiles && ok; ++w) {
+                        const uint32_t s = qs + w, slot = s & 1u;
+                        if (s >= 2) ok = mbar_wait(&q_empty[slot], ((s >> 1) - 1) & 1u, p.status);
+                        if (!ok) break;
+                        mbar_expect_tx(&q_full[slot], (uint32_t)p.tile_tokens * G * HD * 2u);
+                        for (int h = 0; h < HALVES; ++h)
+                            tma_load_4d(qbuf + slot * SM::Q_BYTES + h * SM::Q_HALF, &tmQ, &q_full[slot], 0, h, item.kvh * G, item.q_tok + w * p.tile_tokens);
+                    }
+                }
+                qs += item.tiles;
+                ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
+                if (!ok) break;
+                // page-table entries: the warp holds those of 4 stages (32 pages, one per lane) and fetches the next 32 meanwhile
+                const int* pt = p.page_tables + (size_t)item.req * p.max_pages;
+                const int first_page = item.kv_begin >> 4, last_page = (item.kv_end - 1) >> 4;
+                int ent_cur = first_page + lane <= last_page ? pt[first_page + lane] : 0;
+                int ent_next = first_page + 32 + lane <= last_page ? pt[first_page + 32 + lane] : 0;
+                int k = 0;
+                for (int kv0 = item.kv_begin; kv0 < item.kv_end; kv0 += SHARED_STAGE, ++st, ++k) {
+                    if (k > 0 && (k & 3) == 0) {
+                        ent_cur = ent_next;
+                        const int nidx = first_page + (k >> 2) * 32 + 32 + lane;
+                        ent_next = nidx <= last_page ? pt[nidx] : 0;
+                    }
+                    int page = __shfl_sync(0xFFFFFFFFu, ent_cur, ((k & 3) * SHR_PAGES + (lane & 7)) & 31);
+                    const int npg = min(SHR_PAGES, (item.kv_end - kv0 + 15) >> 4);
+                    if (lane < npg && (unsigned)page >= (unsigned)p.n_pages) {
+                        atomicExch(p.status, 2);
+                        page = 0;
+                    }
+                    const int block = p.layer_block0 + 2 * (page * p.n_kv_heads + item.kvh);
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        const uint32_t n = v ? VS : KS, s = st % n;
+                        uint64_t* full = v ? v_full : k_full;
+                        if (lane == 0) {
+                            if (st >= n) ok = mbar_wait(&(v ? v_empty : k_empty)[s], ((st / n) - 1) & 1u, p.status);
+                            if (ok) mbar_expect_tx(&full[s], (uint32_t)npg * SM::BOX_BYTES);
+                        }
+                        ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
+                        if (!ok) break;
+                        if (lane < npg)
+                            tma_load_5d((v ? vring : kring) + s * SM::K_BYTES + lane * SM::BOX_BYTES, &tmKV, &full[s], 0, 0, 0, 0, block + v);
+                    }
+                    if (!ok) break;
+                }
+            }
+        } else if (warp == SHR_MMA_WARP && elect_one()) {
+            // -------------------------------------------------------- MMA issuer
+            // Each group's stages go Q K^T, P V, Q K^T, ... ; the thread issues whatever is ready, k-steps of both groups in
+            // turn when both are (an MMA into the accumulator of the one before it waits for it, attention2.cuh).
+            constexpr uint32_t QK_STEPS = HD / 16;
+            const uint32_t idesc_pv = umma_idesc_f16_bmn(128, HD);
+            uint32_t st = 0, qs = 0;         // stage and Q slot of the item's first
+            uint32_t use[2] = {0, 0};        // stages of each group in the items before
+            uint32_t o_use[2] = {0, 0};      // items of each group before
+            bool ok = true;
+            for (int it = it_begin; list_ok && it < it_end && ok; ++it) {
+                const SharedItem item = p.items[it];
+                if (!shared_item_ok(item, p)) break;
+                const bool two = item.tiles == 2;
+                const uint32_t n_st = (uint32_t)(item.kv_end - item.kv_begin + SHARED_STAGE - 1) / SHARED_STAGE;
+                const uint32_t n[2] = {two ? n_st : (n_st + 1) / 2, two ? n_st : n_st / 2};
+                uint32_t nq[2] = {0, 0}, np[2] = {0, 0};   // Q K^T and P V issued
+                auto stage_of = [&](int w, uint32_t i) { return two ? i : 2 * i + w; };
+                auto pages_of = [&](uint32_t k) { return (uint32_t)min(SHR_PAGES, (item.kv_end - item.kv_begin - (int)k * SHARED_STAGE + 15) >> 4); };
+                long long t0 = 0;
+                uint32_t idle = 0;
+                while (np[0] < n[0] || np[1] < n[1]) {
+                    int op[2];               // 1: Q K^T, 2: P V
+                    uint32_t steps[2] = {0, 0}, d[2], a_tmem[2], idesc[2];
+                    uint64_t a[2], b[2];
+                    uint32_t at[2];
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        op[w] = 0;
+                        if (nq[w] == np[w] && nq[w] < n[w]) {
+                            const uint32_t s = st + stage_of(w, nq[w]), q = qs + (two ? w : 0);
+                            if (mbar_test(&k_full[s % KS], (s / KS) & 1u) && mbar_test(&q_full[q & 1u], (q >> 1) & 1u)) {
+                                op[w] = 1;
+                                steps[w] = QK_STEPS;
+                                d[w] = tmem_base + 256 + w * 128;
+                                a[w] = umma_desc_k128(smem_u32(qbuf + (q & 1u) * SM::Q_BYTES));
+                                b[w] = umma_desc_k128s(smem_u32(kring + (s % KS) * SM::K_BYTES), SM::GROUP_BYTES);
+                                idesc[w] = umma_idesc_f16(128, 16 * pages_of(s - st));
+                                at[w] = s - st;
+                            }
+                        } else if (np[w] < nq[w]) {
+                            const uint32_t s = st + stage_of(w, np[w]), u = use[w] + np[w];
+                            if (mbar_test(&p_full[w], u & 1u) && mbar_test(&v_full[s % VS], (s / VS) & 1u) &&
+                                (np[w] > 0 || o_use[w] == 0 || mbar_test(&o_empty[w], (o_use[w] - 1) & 1u))) {
+                                op[w] = 2;
+                                steps[w] = pages_of(s - st);
+                                d[w] = tmem_base + w * 128;
+                                a_tmem[w] = tmem_base + 256 + w * 128;
+                                b[w] = umma_desc_mn128(smem_u32(vring + (s % VS) * SM::K_BYTES), 1024, SM::GROUP_BYTES);
+                                idesc[w] = idesc_pv;
+                                at[w] = s - st;
+                            }
+                        }
+                    }
+                    if (!op[0] && !op[1]) {
+                        if ((++idle & 0x3FFu) == 0) {
+                            const long long now = clock64();
+                            if (t0 == 0) t0 = now;
+                            else if (now - t0 > SYN_SPIN_LIMIT_CYCLES) {
+                                atomicExch(p.status, 1);
+                                ok = false;
+                                break;
+                            }
+                        }
+                        continue;
+                    }
+                    idle = 0;
+                    t0 = 0;
+                    tc_fence_after();
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) {
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            if (i >= steps[w]) continue;
+                            if (op[w] == 1)   // step i: 16 dims, of the second half from step 4 on
+                                umma_bf16(d[w], a[w] + (i >> 2) * (SM::Q_HALF >> 4) + 2 * (i & 3), b[w] + (i >> 2) * (1024 >> 4) + 2 * (i & 3), idesc[w], i != 0);
+                            else              // step i: the 16 keys of a page; the item's first P V starts its O afresh
+                                umma_f16_ta(d[w], a_tmem[w] + 8 * i, b[w] + i * (SM::BOX_BYTES >> 4), idesc[w], np[w] != 0 || i != 0);
+                        }
+                    }
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        const uint32_t s = st + at[w];
+                        if (op[w] == 1) {
+                            ++nq[w];
+                            umma_commit(&s_full[w]);
+                            if (!two || nq[w ^ 1] >= nq[w]) umma_commit(&k_empty[s % KS]);   // the other tile has had this stage's K
+                            if (two ? nq[w] == n[w] : nq[0] == n[0] && nq[1] == n[1]) umma_commit(&q_empty[(qs + (two ? w : 0)) & 1u]);
+                        } else if (op[w] == 2) {
+                            ++np[w];
+                            if (!two || np[w ^ 1] >= np[w]) umma_commit(&v_empty[s % VS]);
+                            if (np[w] == n[w]) umma_commit(&o_full[w]);
+                        }
+                    }
+                }
+                st += n_st;
+                qs += item.tiles;
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    use[w] += n[w];
+                    o_use[w] += n[w] > 0;
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------ softmax groups (thread = row)
+        // A wait that runs out sets `ok` = false; the warp then skips all further waits and tensor-memory traffic.
+        reg_alloc<SHR_SOFTMAX_REGS>();
+        const int wg = (warp - 4) >> 2, wq = (warp - 4) & 3, row = wq * 32 + lane;   // group, lane quarter, row of the tile
+        const uint32_t t_lane = tmem_base + ((uint32_t)(wq * 32) << 16);
+        const uint32_t o_col = (uint32_t)wg * 128, s_col = 256 + (uint32_t)wg * 128;
+        uint32_t st = 0, use = 0, o_use = 0;
+        bool ok = true;   // uniform over the warp: the tensor-memory loads and stores are warp-wide
+        auto wait_all = [&](uint64_t* bar, uint32_t parity) {
+            const bool r = mbar_wait(bar, parity, p.status);
+            return __all_sync(0xFFFFFFFFu, r) != 0;
+        };
+        for (int it = it_begin; list_ok && it < it_end; ++it) {
+            const SharedItem item = p.items[it];
+            if (!shared_item_ok(item, p)) {   // uniform over the CTA
+                if (threadIdx.x == 128) atomicExch(p.status, 2);
+                break;
+            }
+            const bool two = item.tiles == 2;
+            const int first_tok = two ? wg * p.tile_tokens : 0;       // of the group's tile, within the item
+            const int rows = (two && wg == 0 ? p.tile_tokens : item.n_tok - first_tok) * G;
+            const bool live = row < rows;
+            const bool wlive = wq * 32 < rows;   // a warp none of whose rows exist only keeps the barriers' counts
+            const int n_st = (item.kv_end - item.kv_begin + SHARED_STAGE - 1) / SHARED_STAGE;
+            const int lim = item.q_pos0 + first_tok + row / G;        // last visible key position of this row
+            float m_used = -INFINITY, l = 0.f;
+            int mine = 0;                                             // stages of this group
+            for (int k = 0; k < n_st; ++k) {
+                if (!two && (k & 1) != wg) continue;
+                const int kv0 = item.kv_begin + k * SHARED_STAGE;
+                if (ok) ok = wait_all(&s_full[wg], use & 1u);
+                ++use;
+                if (wlive && ok) {
+                    uint32_t s[4][32];
+                    tc_fence_after();
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld32(t_lane + s_col + 32 * c, s[c]);
+                    tmem_ld_wait();
+                    // keys this row sees in the stage: positions < min(kv_end, lim + 1)
+                    const int nvalid = min(item.kv_end, lim + 1) - kv0;
+                    if (nvalid < SHARED_STAGE) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (32 * c + i >= nvalid) s[c][i] = 0xFF800000u;   // -inf
+                    }
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(s[c][i]));
+                    const float ms = mx * p.scale_log2;
+                    if (mine == 0) {
+                        m_used = live ? ms : 0.f;
+                    } else {
+                        const bool grow = live && ms > m_used + ATT2_RESCALE_GAP;
+                        if (__any_sync(0xFFFFFFFFu, grow)) {
+                            const float corr = grow ? ex2_approx(m_used - ms) : 1.f;   // (P V of the stage before is complete: s_full)
+                            if (grow) {
+                                m_used = ms;
+                                l *= corr;
+                            }
+#pragma unroll 1
+                            for (int ch = 0; ch < HD / 16; ++ch) {
+                                uint32_t o[16];
+                                tmem_ld16(t_lane + o_col + ch * 16, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * corr);
+                                tmem_st16(t_lane + o_col + ch * 16, o);
+                            }
+                        }
+                    }
+                    const float base = (m_used == -INFINITY ? 0.f : m_used) - SHR_P_SCALE_LOG2;
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t pw[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float a = ex2_approx(fmaf(__uint_as_float(s[c][2 * i]), p.scale_log2, -base));
+                            const float b = ex2_approx(fmaf(__uint_as_float(s[c][2 * i + 1]), p.scale_log2, -base));
+                            sum[i & 3] += a + b;
+                            pw[i] = pack_op(a, b);   // (rows beyond the tile's hold garbage: they only meet themselves in the products)
+                        }
+                        tmem_st16(t_lane + s_col + 16 * c, pw);
+                    }
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    tmem_st_wait();
+                    tc_fence_before();
+                }
+                // Rows of the last page behind the item's keys: a weight of zero takes whatever is stale there out, unless that is no
+                // number.  Every group that uses the stage clears them before its P V can start.
+                if ((item.kv_end & 15) && k == n_st - 1 && ok) {
+                    const uint32_t vs = (st + k) % VS;
+                    ok = wait_all(&v_full[vs], ((st + k) / VS) & 1u);
+                    uint8_t* box = vring + vs * SM::K_BYTES + ((item.kv_end - 1 - kv0) >> 4) * SM::BOX_BYTES;
+                    const int r0 = item.kv_end & 15;
+                    for (int c = row; ok && c < (16 - r0) * HALVES * 8; c += 128) {
+                        const int r = r0 + c / (HALVES * 8), h = (c >> 3) % HALVES;
+                        *reinterpret_cast<uint4*>(box + (r >> 3) * SM::GROUP_BYTES + h * 1024 + (r & 7) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                }
+                __syncwarp();
+                if (lane == 0 && ok) mbar_arrive(&p_full[wg]);
+                ++mine;
+            }
+            st += n_st;
+            if (mine == 0) continue;   // one tile, one stage: the second group has no part in it
+            // ---- end of the item: the fp32 partial (m, l, O) of the group's rows
+            if (ok) ok = wait_all(&o_full[wg], o_use & 1u);
+            ++o_use;
+            if (ok && wlive) {
+                tc_fence_after();
+                const int64_t at = (int64_t)item.base + (two ? first_tok * G : wg * item.n_tok * G) + row;
+#pragma unroll 1
+                for (int ch = 0; ch < HD / 32; ++ch) {
+                    uint32_t o[32];
+                    tmem_ld32(t_lane + o_col + ch * 32, o);
+                    tmem_ld_wait();
+                    if (live) {
+                        uint4* dst = reinterpret_cast<uint4*>(p.part_o + at * HD + ch * 32);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) dst[c] = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                    }
+                }
+                tc_fence_before();
+                if (live) p.part_ml[at] = make_float2((m_used == -INFINITY ? 0.f : m_used) - SHR_P_SCALE_LOG2, l);
+            }
+            __syncwarp();
+            if (lane == 0 && ok) mbar_arrive(&o_empty[wg]);
+        }
+    }
+    // ---------------------------------------------------------------- teardown
+    tc_fence_before();
+    __syncthreads();
+    if (warp == SHR_MMA_WARP) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, SM::TMEM_COLS);
+    }
+}
+
+// Joins the partials of a (token, query head), one warp each: the lanes read 32 parts' (m, l) at a time, then O part by part.
+template <int HD>
+__global__ void __launch_bounds__(128)
+shared_merge_kernel(SharedParams p, int n_rows_out) {
+    constexpr int E = HD / 32;   // components of a lane
+    const int r = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    pdl_launch_dependents();
+    pdl_wait();
+    if (r >= n_rows_out) return;
+    const int n_q_heads = p.n_kv_heads * p.group, t = r / n_q_heads, hq = r - t * n_q_heads, kvh = hq / p.group;
+    const int seg = p.seg_of_token[t];
+    const int off = (t - p.seg_first[seg]) * p.group + hq - kvh * p.group;
+    const int* li = p.list_begin + seg * p.n_kv_heads + kvh;
+    const int b = li[0], e = li[1];
+    float m = -INFINITY, sum = 0.f, acc[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) acc[i] = 0.f;
+    for (int k0 = b; k0 < e; k0 += 32) {
+        const int n = min(32, e - k0);
+        int at = 0;
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (lane < n) {
+            at = p.list[k0 + lane] + off;
+            if ((unsigned)at < (unsigned)p.n_rows) ml = __ldcg(&p.part_ml[at]);
+            else {
+                atomicExch(p.status, 2);
+                at = 0;
+            }
+        }
+        float mk = ml.y > 0.f || isnan(ml.y) ? ml.x : -INFINITY;   // a part in which the row sees nothing has no say
+        float mn = mk;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, o));
+        mn = fmaxf(m, mn);
+        const float bs = mn == -INFINITY ? 0.f : mn, corr = ex2_approx(m - bs);
+        const float w = ex2_approx(mk - bs);
+        float ws = w > 0.f ? w * ml.y : 0.f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) ws += __shfl_xor_sync(0xFFFFFFFFu, ws, o);
+        sum = sum * corr + ws;
+#pragma unroll
+        for (int i = 0; i < E; ++i) acc[i] *= corr;
+        m = mn;
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) {
+            const float wk = __shfl_sync(0xFFFFFFFFu, w, k);
+            const int ak = __shfl_sync(0xFFFFFFFFu, at, k);
+            const float* src = p.part_o + (int64_t)ak * HD + lane * E;
+            float v[E];
+            if constexpr (E == 4) {
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(src));
+                v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+            } else {
+                const float2 x = __ldcg(reinterpret_cast<const float2*>(src));
+                v[0] = x.x; v[1] = x.y;
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) acc[i] = wk > 0.f ? fmaf(v[i], wk, acc[i]) : acc[i];
+        }
+    }
+    const float inv = 1.f / sum;
+    uint32_t o[E / 2];
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) o[i] = pack_op(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+    op16* dst = p.out + (int64_t)t * p.q_dim + hq * HD + lane * E;
+    if constexpr (E == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(o[0], o[1]);
+    else *reinterpret_cast<uint32_t*>(dst) = o[0];
+}
+
+}  // namespace syn

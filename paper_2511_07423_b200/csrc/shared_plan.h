@@ -1,0 +1,190 @@
+// The host planner of attention over shared prefixes (no device): which keys which query tokens meet together, cut into work
+// items of equal time, and where the items' partial results lie.
+//
+// Requests next to each other in the batch whose page tables begin with the same pages, all of them full and cached for either,
+// share those keys.  The common pages of neighbours form a tree: a run of requests, its common prefix, and within the run
+// shorter runs that have more in common.  Every node is one set of (tokens of the run) x (keys beyond the parent's); a leaf
+// is a request with what only it sees, its chunk among that.  A token's keys are those of its path from the root, each once.
+#pragma once
+#include <stdint.h>
+
+#include <algorithm>
+#include <vector>
+
+namespace syn {
+
+constexpr int SHARED_STAGE = 128;        // keys of a stage
+constexpr int SHARED_TILE_ROWS = 128;    // rows (token, query head of the kv head) of a tile; an item has one tile or two
+constexpr int SHARED_NO_LIMIT = 0x3FFFFFFF;   // q_pos0 of an item whose rows see all of its keys
+
+struct SharedItem {
+    int q_tok, n_tok;        // query tokens
+    int kvh, req;            // kv head; the request whose page table names the keys
+    int kv_begin, kv_end;    // keys (the first a multiple of 16)
+    int q_pos0;              // token j sees keys <= q_pos0 + j
+    int base;                // its first row of partial results: row (j, g) at base + j * G + g
+    int tiles;               // 2: two tiles, each over every stage; 1: one tile, two groups of warps over alternate stages, the second's
+                             // results n_tok * G rows behind the first's (if there is a second stage)
+    int pad0, pad1, pad2;
+};
+
+// Cycles of a stage, of an item, of a launch (see shared_plan).
+struct SharedCost { int stage1, stage2, item, fixed; };
+
+struct SharedPlan {
+    bool shares = false;                 // some keys are met by several requests' tokens
+    int n_cta = 0;
+    int64_t rows = 0;                    // rows of partial results
+    int64_t estimate = 0;                // cycles
+    int64_t kv_keys = 0;                 // keys read, each node's once (per kv head)
+    std::vector<SharedItem> items;       // by CTA
+    std::vector<int> cta_begin;
+    // where a token's partial results are: segment of the token; of (segment, kv head) the rows of the segment's first token
+    std::vector<int> seg_of_token, seg_first, list_begin, list;
+};
+
+struct SharedNode { int a, b, from, to; };   // requests [a, b), pages [from, to); to < 0: the leaf of request a
+
+// The tree, as the list of its nodes; least: pages from which on a common prefix is worth a node.
+inline std::vector<SharedNode> shared_tree(int n_req, const int* page_tables, int max_pages, const int* ctx_lens, int page_size, int least) {
+    std::vector<int> common(n_req, 0);       // pages that i and i + 1 share
+    for (int i = 0; i + 1 < n_req; ++i) {
+        const int most = std::min(ctx_lens[i], ctx_lens[i + 1]) / page_size;
+        const int *p = page_tables + (size_t)i * max_pages, *q = p + max_pages;
+        int k = 0;
+        while (k < most && p[k] == q[k]) ++k;
+        common[i] = k;
+    }
+    std::vector<SharedNode> nodes;
+    struct Run { int a, b, from; };
+    std::vector<Run> todo = {{0, n_req, 0}};
+    while (!todo.empty()) {
+        const Run r = todo.back();
+        todo.pop_back();
+        if (r.b - r.a == 1) {
+            nodes.push_back({r.a, r.b, r.from, -1});
+            continue;
+        }
+        const int s = *std::min_element(common.begin() + r.a, common.begin() + r.b - 1);
+        int from = r.from;
+        if (s - from >= least) {
+            nodes.push_back({r.a, r.b, from, s});
+            from = s;
+        }
+        int end = r.b;                        // pushed back to front: taken front to back
+        for (int i = r.b - 2; i >= r.a; --i)
+            if (common[i] == s) {
+                todo.push_back({i + 1, end, from});
+                end = i + 1;
+            }
+        todo.push_back({r.a, end, from});
+    }
+    return nodes;
+}
+
+inline void shared_plan(int n_req, const int* chunk_offsets, const int* page_tables, int max_pages, const int* ctx_lens, int page_size,
+                        int group, int n_kv_heads, int n_sm, const SharedCost& cost, SharedPlan& sp) {
+    const std::vector<SharedNode> nodes = shared_tree(n_req, page_tables, max_pages, ctx_lens, page_size, SHARED_STAGE / page_size);
+    const int T = chunk_offsets[n_req], tile_tokens = SHARED_TILE_ROWS / group;
+    // units: a node's tokens in items of at most two tiles
+    struct Unit { int q_tok, n_tok, req, kv_begin, kv_end, q_pos0, tiles, stages; int64_t stage; };
+    std::vector<Unit> units;
+    std::vector<int> cuts = {0, T};
+    for (const SharedNode& nd : nodes) {
+        const bool leaf = nd.to < 0;
+        const int t0 = chunk_offsets[nd.a], t1 = chunk_offsets[nd.b];
+        const int kv0 = nd.from * page_size, kv1 = leaf ? ctx_lens[nd.a] + (t1 - t0) : nd.to * page_size;
+        sp.shares = sp.shares || !leaf;
+        sp.kv_keys += kv1 - kv0;
+        for (int t = t0; t < t1; t += 2 * tile_tokens) {
+            const int n = std::min(2 * tile_tokens, t1 - t);
+            // a leaf's tokens see keys up to their own position; those of its first tiles need not read what only later ones see
+            const int end = leaf ? ctx_lens[nd.a] + (t - t0) + n : kv1;
+            Unit u = {t, n, nd.a, kv0, end, leaf ? ctx_lens[nd.a] + (t - t0) : SHARED_NO_LIMIT, n > tile_tokens ? 2 : 1, (end - kv0 + SHARED_STAGE - 1) / SHARED_STAGE, 0};
+            u.stage = u.tiles == 2 ? cost.stage2 : cost.stage1;
+            units.push_back(u);
+            cuts.push_back(t);
+            cuts.push_back(t + n);
+        }
+    }
+    std::stable_sort(units.begin(), units.end(), [](const Unit& x, const Unit& y) { return x.stages * x.stage > y.stages * y.stage; });
+    int64_t total = 0, longest = 0;
+    for (const Unit& u : units) {
+        total += (u.stages * u.stage + cost.item) * n_kv_heads;
+        longest = std::max(longest, u.stages * u.stage + cost.item);
+    }
+    // The units one after the other, longest first, each CTA filled up to `limit`; what does not fit goes on in the next CTA.
+    auto fill = [&](int64_t limit, auto&& emit) {
+        int cta = 0;
+        int64_t load = 0;
+        for (const Unit& u : units)
+            for (int h = 0; h < n_kv_heads; ++h)
+                for (int at = 0; at < u.stages;) {
+                    const int64_t room = (limit - load - cost.item) / u.stage;
+                    int take = (int)std::min<int64_t>(u.stages - at, std::max<int64_t>(room, 0));
+                    if (take < u.stages - at && take < 2) take = 0;      // no slivers
+                    if (take == 0 && load == 0) return false;
+                    if (take) {
+                        emit(u, h, at, at + take, cta);
+                        load += take * u.stage + cost.item;
+                        at += take;
+                    }
+                    if (at < u.stages) {
+                        load = 0;
+                        if (++cta >= n_sm) return false;
+                    }
+                }
+        return true;
+    };
+    auto nothing = [](const Unit&, int, int, int, int) {};
+    int64_t lo = total / n_sm, hi = std::max(lo, longest);
+    while (!fill(hi, nothing)) hi += hi / 4;
+    while (hi - lo > 64 + lo / 128) {
+        const int64_t mid = (lo + hi) / 2;
+        if (fill(mid, nothing)) hi = mid; else lo = mid;
+    }
+    sp.estimate = hi + cost.fixed;
+    std::vector<int> owner;
+    // parts of (unit, head), for the lists below
+    struct Part { int unit, h, base, second; };
+    std::vector<Part> parts;
+    fill(hi, [&](const Unit& u, int h, int s0, int s1, int cta) {
+        const int rows = u.n_tok * group, copies = u.tiles == 1 && s1 - s0 > 1 ? 2 : 1;
+        sp.items.push_back({u.q_tok, u.n_tok, h, u.req, u.kv_begin + s0 * SHARED_STAGE, std::min(u.kv_end, u.kv_begin + s1 * SHARED_STAGE), u.q_pos0,
+                            (int)sp.rows, u.tiles, 0, 0, 0});
+        parts.push_back({(int)(&u - units.data()), h, (int)sp.rows, copies == 2 ? (int)sp.rows + rows : -1});
+        sp.rows += (int64_t)rows * copies;
+        owner.push_back(cta);
+    });
+    sp.n_cta = owner.back() + 1;
+    sp.cta_begin.assign(sp.n_cta + 1, 0);
+    for (int k : owner) sp.cta_begin[k + 1]++;
+    for (int k = 0; k < sp.n_cta; ++k) sp.cta_begin[k + 1] += sp.cta_begin[k];
+    // segments: tokens between two cuts belong to the same units
+    std::sort(cuts.begin(), cuts.end());
+    cuts.erase(std::unique(cuts.begin(), cuts.end()), cuts.end());
+    const int n_seg = (int)cuts.size() - 1;
+    sp.seg_of_token.resize(T);
+    sp.seg_first.assign(cuts.begin(), cuts.end() - 1);
+    for (int s = 0; s < n_seg; ++s)
+        for (int t = cuts[s]; t < cuts[s + 1]; ++t) sp.seg_of_token[t] = s;
+    sp.list_begin.assign((size_t)n_seg * n_kv_heads + 1, 0);
+    auto each = [&](auto&& f) {
+        for (const Part& p : parts) {
+            const Unit& u = units[p.unit];
+            for (int s = sp.seg_of_token[u.q_tok]; s < n_seg && cuts[s] < u.q_tok + u.n_tok; ++s) f(p, u, s);
+        }
+    };
+    each([&](const Part& p, const Unit&, int s) { sp.list_begin[(size_t)s * n_kv_heads + p.h + 1] += p.second >= 0 ? 2 : 1; });
+    for (size_t k = 0; k + 1 < sp.list_begin.size(); ++k) sp.list_begin[k + 1] += sp.list_begin[k];
+    sp.list.resize(sp.list_begin.back());
+    std::vector<int> at(sp.list_begin.begin(), sp.list_begin.end() - 1);
+    each([&](const Part& p, const Unit& u, int s) {
+        const int off = (cuts[s] - u.q_tok) * group;
+        int& k = at[(size_t)s * n_kv_heads + p.h];
+        sp.list[k++] = p.base + off;
+        if (p.second >= 0) sp.list[k++] = p.second + off;
+    });
+}
+
+}  // namespace syn

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "attention2.cuh"
+#include "attention_shared.cuh"
 #include "attention_thin.cuh"
 #include "gemm.cuh"
 #include "gemm2.cuh"
@@ -33,7 +34,8 @@ static long long g_spin_limit = SYN_SPIN_LIMIT_CYCLES;
 // 0: every projection takes the kernel its shape calls for; 1: the one-CTA kernel always (syn_debug_set_schedule).
 static int g_schedule = 0;
 // Attention kernel: 0 = whichever the planner makes cheaper for the batch, 1 = warp-level MMAs (64-row tiles),
-// 2 = tcgen05 (128-row tiles), 3 = warp-level MMAs in CTAs of half an SM.
+// 2 = tcgen05 (128-row tiles), 3 = warp-level MMAs in CTAs of half an SM; 4 = plans of syn_plan_create_shared take the
+// shared-prefix kernel whatever the estimates (others as with 0).
 static int g_attention = 0;
 
 // Name of the last CUDA error a call of this library met on this thread (for syn_last_cuda_error).
@@ -358,8 +360,8 @@ struct syn_kv {
 };
 
 // The attention kernels a work list can be made for.
-enum { ATTN_WARP = 1, ATTN_TENSOR = 2, ATTN_THIN = 3 };
-static int attn_rows(int kind) { return kind == ATTN_TENSOR ? 128 : kind == ATTN_THIN ? ATTN_THIN_ROWS : 64; }
+enum { ATTN_WARP = 1, ATTN_TENSOR = 2, ATTN_THIN = 3, ATTN_SHARED = 4 };
+static int attn_rows(int kind) { return kind == ATTN_TENSOR || kind == ATTN_SHARED ? 128 : kind == ATTN_THIN ? ATTN_THIN_ROWS : 64; }
 
 struct syn_plan {
     syn_step_stats stats;
@@ -372,6 +374,11 @@ struct syn_plan {
     size_t o_tokens, o_pos, o_slot, o_offsets, o_uncached, o_tables, o_items, o_cta, o_groups;
     size_t o_row, o_first;   // the judging rows, and where a request's begin among them
     int n_judging = 0;       // rows whose argmax verification looks at: a request's from its last uncached token on
+    // attention over shared prefixes (ATTN_SHARED): the work list's and the merge's arrays, and the plan's own partials
+    size_t o_seg, o_seg_first, o_list_begin, o_list;
+    int n_rows = 0, n_list = 0, n_seg = 0;
+    float* part_o = nullptr;
+    float2* part_ml = nullptr;
     // the cache the page ids and slots were validated against
     const syn_kv* kv = nullptr;
     const void* kv_pool = nullptr;
@@ -487,6 +494,8 @@ static cudaError_t set_kernel_attributes() {
         projection_smem<EPI_PLAIN>(), projection_smem<EPI_QKV>(), projection_smem<EPI_RESID>(), projection_smem<EPI_SWIGLU>(), projection_smem<EPI_LMHEAD>(),
         kernel_smem(attn_kernel<128>, AttnSmem<128>::TOTAL), kernel_smem(attn_kernel<64>, AttnSmem<64>::TOTAL),
         kernel_smem(attn2_kernel<128>, Attn2Smem<128>::TOTAL), kernel_smem(attn2_kernel<64>, Attn2Smem<64>::TOTAL),
+        kernel_smem(attn_shared_kernel<128>, SharedSmem<128>::TOTAL), kernel_smem(attn_shared_kernel<64>, SharedSmem<64>::TOTAL),
+        kernel_smem(shared_merge_kernel<128>, 0), kernel_smem(shared_merge_kernel<64>, 0),
         kernel_smem(attn_thin_kernel<128>, AttnThinSmem<128>::TOTAL), kernel_smem(attn_thin_kernel<64>, AttnThinSmem<64>::TOTAL),
         kernel_smem(prep_kernel, 0), kernel_smem(verify_kernel, 0), kernel_smem(judging_rows_kernel, 0), kernel_smem(topk_rows_kernel, 0), kernel_smem(sample_verify_kernel, 0)};
     for (cudaError_t e : all)
@@ -808,6 +817,8 @@ static int syn_kv_export_impl(syn_kv* kv, uint32_t layer, const int32_t* page_ta
 extern "C" void syn_plan_free(syn_plan* p) {
     if (!p) return;
     cudaFree(p->dev);
+    cudaFree(p->part_o);
+    cudaFree(p->part_ml);
     if (p->host) cudaFreeHost(p->host);
     delete p;
 }
@@ -823,6 +834,7 @@ struct HostPlan {
     std::vector<int> pos, slot, cta_begin;
     std::vector<AttnItem> items;          // sorted by CTA
     std::vector<MergeGroup> groups;
+    int64_t estimate = 0;                 // of the attention of a layer, SM cycles
     syn_step_stats stats;
 };
 
@@ -1057,6 +1069,7 @@ static int plan_compute(const syn_model_desc& c, int P, uint32_t n_pages, int n_
     }
     const int kind = lay.ac->kind;
     hp.kind = kind;
+    hp.estimate = lay.estimate;
     // Positions that no chunk of the batch writes, for the kernel that requests keys before the chunks' are written: up
     // to the first page of the request that holds a written slot, of whichever request.
     std::vector<int> safe;
@@ -1242,16 +1255,53 @@ static int plan_compute(const syn_model_desc& c, int P, uint32_t n_pages, int n_
     return SYN_OK;
 }
 
-// plan_compute, then pack everything into the plan's pinned buffer (grown on demand).
+// The attention kernel that plans are laid out for unless they share prefixes (0: the planner's choice).
+static int attention_choice() { return g_attention == ATTN_SHARED ? 0 : g_attention; }
+
+// SM cycles of the shared-prefix kernel: a stage of 128 keys with one tile of rows and with two, an item, a launch with its merge.
+static SharedCost shared_cost(const syn_model_desc& c) {
+    return c.head_dim == 128 ? SharedCost{2400, 3600, 4000, 14000} : SharedCost{1600, 2600, 4000, 14000};
+}
+
+// Whether a batch planned as `hp` is better off with its common prefixes met once; fills `sp`.
+static bool shared_better(const syn_model_desc& c, int P, int n_sm, int32_t n_req, const int32_t* chunk_offsets, const int32_t* page_tables,
+                          int32_t max_pages, const int32_t* ctx_lens, const HostPlan& hp, SharedPlan& sp) {
+    if (g_attention != 0 && g_attention != ATTN_SHARED) return false;
+    shared_plan(n_req, chunk_offsets, page_tables, max_pages, ctx_lens, P, c.n_q_heads / c.n_kv_heads, c.n_kv_heads, n_sm, shared_cost(c), sp);
+    if (sp.rows > (int64_t)1 << 30) return false;
+    return g_attention == ATTN_SHARED || (sp.shares && sp.estimate < hp.estimate);
+}
+
+// The step's counters of a batch whose attention runs over shared prefixes: every shared key is read once.
+static void shared_stats(const syn_model_desc& c, const SharedPlan& sp, syn_step_stats& s) {
+    s.kv_read_bytes = sp.kv_keys * (int64_t)(2 * c.n_kv_heads * c.head_dim * 2) * c.n_layers;
+    s.attn_items = s.attn_split_items = (int)sp.items.size();
+    s.kernel_launches += c.n_layers;   // the merge
+    s.attn_rows = attn_rows(ATTN_SHARED);
+}
+
+// plan_compute, then pack everything into the plan's pinned buffer (grown on demand).  share: prefixes that neighbours have in
+// common may be met once.
 static int plan_build(syn_plan* p, syn_model* m, syn_kv* kv, int32_t n_req, const int32_t* chunk_tokens,
                       const int32_t* chunk_offsets, const int32_t* page_tables, int32_t max_pages, const int32_t* ctx_lens,
-                      const int32_t* n_uncached) {
+                      const int32_t* n_uncached, bool share = false) {
     if (!m || !kv || kv->model != m) return SYN_E_INVALID_ARG;
     HostPlan hp;
     int r = plan_compute(m->desc, (int)kv->page_size, kv->n_pages, m->n_sm, n_req, chunk_tokens, chunk_offsets, page_tables,
-                         max_pages, ctx_lens, n_uncached, g_attention, thin_attention_ctas(m->n_sm), hp);
+                         max_pages, ctx_lens, n_uncached, attention_choice(), thin_attention_ctas(m->n_sm), hp);
     if (r) return r;
-    const int T = hp.T, n_items = (int)hp.items.size(), n_cta = hp.n_cta;
+    SharedPlan sp;
+    const bool shared = share && shared_better(m->desc, (int)kv->page_size, m->n_sm, n_req, chunk_offsets, page_tables, max_pages, ctx_lens, hp, sp);
+    if (shared) {
+        hp.kind = ATTN_SHARED;
+        hp.items.clear(); hp.groups.clear();
+        hp.n_parts = 0;
+        hp.n_cta = sp.n_cta;
+        hp.cta_begin = sp.cta_begin;
+        shared_stats(m->desc, sp, hp.stats);
+    }
+    const int T = hp.T, n_items = (int)(shared ? sp.items.size() : hp.items.size()), n_cta = hp.n_cta;
+    const size_t item_bytes = shared ? sizeof(SharedItem) : sizeof(AttnItem);
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
     p->o_tokens = take((size_t)T * 4);
@@ -1262,9 +1312,13 @@ static int plan_build(syn_plan* p, syn_model* m, syn_kv* kv, int32_t n_req, cons
     p->o_tables = take((size_t)n_req * max_pages * 4);
     p->o_row = take((size_t)T * 4);
     p->o_first = take((size_t)n_req * 4);
-    p->o_items = take((size_t)n_items * sizeof(AttnItem));
+    p->o_items = take((size_t)n_items * item_bytes);
     p->o_cta = take((size_t)(n_cta + 1) * 4);
     p->o_groups = take(std::max<size_t>(1, hp.groups.size()) * sizeof(MergeGroup));
+    p->o_seg = take(sp.seg_of_token.size() * 4);
+    p->o_seg_first = take(sp.seg_first.size() * 4);
+    p->o_list_begin = take(sp.list_begin.size() * 4);
+    p->o_list = take(sp.list.size() * 4);
     if (off > p->cap) {
         cudaFree(p->dev);
         if (p->host) cudaFreeHost(p->host);
@@ -1288,9 +1342,18 @@ static int plan_build(syn_plan* p, syn_model* m, syn_kv* kv, int32_t n_req, cons
         for (int t = chunk_offsets[i] + u - 1; t < chunk_offsets[i + 1]; ++t) p->h<int>(p->o_row)[p->n_judging++] = t;
     }
     memcpy(p->h<int>(p->o_tables), page_tables, (size_t)n_req * max_pages * 4);
-    memcpy(p->h<AttnItem>(p->o_items), hp.items.data(), (size_t)n_items * sizeof(AttnItem));
+    memcpy(p->h<uint8_t>(p->o_items), shared ? (const void*)sp.items.data() : (const void*)hp.items.data(), (size_t)n_items * item_bytes);
     memcpy(p->h<int>(p->o_cta), hp.cta_begin.data(), (size_t)(n_cta + 1) * 4);
     if (!hp.groups.empty()) memcpy(p->h<MergeGroup>(p->o_groups), hp.groups.data(), hp.groups.size() * sizeof(MergeGroup));
+    if (shared) {
+        memcpy(p->h<int>(p->o_seg), sp.seg_of_token.data(), sp.seg_of_token.size() * 4);
+        memcpy(p->h<int>(p->o_seg_first), sp.seg_first.data(), sp.seg_first.size() * 4);
+        memcpy(p->h<int>(p->o_list_begin), sp.list_begin.data(), sp.list_begin.size() * 4);
+        memcpy(p->h<int>(p->o_list), sp.list.data(), sp.list.size() * 4);
+        p->n_rows = (int)sp.rows; p->n_list = (int)sp.list.size(); p->n_seg = (int)sp.seg_first.size();
+        CU_OK(cudaMalloc(&p->part_o, (size_t)sp.rows * m->desc.head_dim * 4));
+        CU_OK(cudaMalloc(&p->part_ml, (size_t)sp.rows * 8));
+    }
     p->n_req = n_req; p->T = T; p->max_pages = max_pages; p->n_items = n_items; p->n_cta = n_cta;
     p->n_groups = (int)hp.groups.size(); p->n_parts = hp.n_parts;
     p->attn = hp.kind;
@@ -1310,7 +1373,7 @@ static int plan_host(const syn_model_desc* desc, uint32_t n_pages, uint32_t page
     if (desc->n_kv_heads == 0 || desc->n_q_heads % desc->n_kv_heads != 0 || desc->n_q_heads / desc->n_kv_heads > 8)
         return SYN_E_INVALID_ARG;
     int r = plan_compute(*desc, (int)page_size, n_pages, n_sm, n_req, chunk_tokens, chunk_offsets, page_tables, max_pages,
-                         ctx_lens, n_uncached, g_attention, thin_ctas, hp);
+                         ctx_lens, n_uncached, attention_choice(), thin_ctas, hp);
     if (r) return r;
     *n_items = (int)hp.items.size();
     *n_cta = hp.n_cta;
@@ -1361,11 +1424,11 @@ static int syn_plan_work_host_impl(const syn_model_desc* desc, uint32_t n_pages,
 
 static int syn_plan_create_impl(syn_model* m, syn_kv* kv, int32_t n_req, const int32_t* chunk_tokens,
                                const int32_t* chunk_offsets, const int32_t* page_tables, int32_t max_pages,
-                               const int32_t* ctx_lens, const int32_t* n_uncached, syn_plan** out) {
+                               const int32_t* ctx_lens, const int32_t* n_uncached, bool share, syn_plan** out) {
     if (!out) return SYN_E_INVALID_ARG;
     syn_plan* p = new (std::nothrow) syn_plan();
     if (!p) return SYN_E_OOM;
-    int r = plan_build(p, m, kv, n_req, chunk_tokens, chunk_offsets, page_tables, max_pages, ctx_lens, n_uncached);
+    int r = plan_build(p, m, kv, n_req, chunk_tokens, chunk_offsets, page_tables, max_pages, ctx_lens, n_uncached, share);
     if (r == SYN_OK) {
         cudaError_t e = cudaMemcpy(p->dev, p->host, p->used, cudaMemcpyHostToDevice);
         if (e != cudaSuccess) r = SYN_E_CUDA;
@@ -1376,6 +1439,53 @@ static int syn_plan_create_impl(syn_model* m, syn_kv* kv, int32_t n_req, const i
         return r;
     }
     *out = p;
+    return SYN_OK;
+}
+
+static int syn_plan_shared_host_impl(const syn_model_desc* desc, uint32_t n_pages, uint32_t page_size, int32_t n_sm, int32_t n_req,
+                                     const int32_t* chunk_tokens, const int32_t* chunk_offsets, const int32_t* page_tables, int32_t max_pages,
+                                     const int32_t* ctx_lens, const int32_t* n_uncached, int32_t* items, int32_t items_cap, int32_t* n_items,
+                                     int32_t* cta_begin, int32_t* n_cta, int32_t* parts, int32_t parts_cap, int32_t* n_parts, int32_t* taken,
+                                     syn_step_stats* stats) {
+    if (!n_items || !n_cta || !n_parts || !taken || n_sm <= 0 || n_sm > 32767) return SYN_E_INVALID_ARG;
+    HostPlan hp;
+    int dummy_items = 0, dummy_ctas = 0;
+    const int r = plan_host(desc, n_pages, page_size, n_sm, thin_attention_ctas(n_sm), n_req, chunk_tokens, chunk_offsets, page_tables, max_pages,
+                            ctx_lens, n_uncached, nullptr, 0, SYN_PLAN_ITEM_FIELDS, &dummy_items, nullptr, &dummy_ctas, hp);
+    if (r) return r;
+    SharedPlan sp;
+    *taken = shared_better(*desc, (int)page_size, n_sm, n_req, chunk_offsets, page_tables, max_pages, ctx_lens, hp, sp) ? 1 : 0;
+    if (sp.items.empty())   // another kernel was asked for
+        shared_plan(n_req, chunk_offsets, page_tables, max_pages, ctx_lens, (int)page_size, desc->n_q_heads / desc->n_kv_heads, desc->n_kv_heads, n_sm, shared_cost(*desc), sp);
+    *n_items = (int)sp.items.size();
+    *n_cta = sp.n_cta;
+    // (token, kv head) by (token, kv head): the rows of its partial results
+    const int Hkv = desc->n_kv_heads, G = desc->n_q_heads / Hkv;
+    int64_t count = 0;
+    for (int t = 0; t < hp.T; ++t) {
+        const int s = sp.seg_of_token[t];
+        for (int h = 0; h < Hkv; ++h)
+            for (int k = sp.list_begin[(size_t)s * Hkv + h]; k < sp.list_begin[(size_t)s * Hkv + h + 1]; ++k, ++count)
+                if (parts && count < parts_cap) {
+                    const int32_t row[3] = {t, h, sp.list[k] + (t - sp.seg_first[s]) * G};
+                    memcpy(parts + 3 * count, row, sizeof(row));
+                }
+    }
+    if (count > INT32_MAX) return SYN_E_CAPACITY;
+    *n_parts = (int32_t)count;
+    if ((items && items_cap < *n_items) || (parts && parts_cap < *n_parts)) return SYN_E_CAPACITY;
+    if (items)
+        for (int i = 0; i < *n_items; ++i) {
+            const SharedItem& it = sp.items[i];
+            const int32_t row[SYN_SHARED_ITEM_FIELDS] = {it.q_tok, it.n_tok, it.kvh, it.req, it.kv_begin, it.kv_end,
+                                                         it.q_pos0 == SHARED_NO_LIMIT ? -1 : it.q_pos0, it.base, it.tiles};
+            memcpy(items + (size_t)i * SYN_SHARED_ITEM_FIELDS, row, sizeof(row));
+        }
+    if (cta_begin) memcpy(cta_begin, sp.cta_begin.data(), (size_t)(sp.n_cta + 1) * 4);
+    if (stats) {
+        *stats = hp.stats;
+        shared_stats(*desc, sp, *stats);
+    }
     return SYN_OK;
 }
 
@@ -1832,8 +1942,52 @@ static cudaError_t attention_kernel(const syn_model* m, const syn_kv* kv, const 
     }
 }
 
+// Attention over shared prefixes: the work list's partials, in the plan's own arrays, then their merge.
+static int launch_shared(syn_model* m, syn_kv* kv, const syn_plan* p, uint32_t layer, const op16* q, op16* out, cudaStream_t st) {
+    const syn_model_desc& c = m->desc;
+    const uint32_t G = c.n_q_heads / c.n_kv_heads, q_dim = c.n_q_heads * c.head_dim;
+    SharedParams sp;
+    memset(&sp, 0, sizeof(sp));
+    sp.items = p->d<SharedItem>(p->o_items);
+    sp.cta_begin = p->d<int>(p->o_cta);
+    sp.page_tables = p->d<int>(p->o_tables);
+    sp.max_pages = p->max_pages; sp.n_kv_heads = c.n_kv_heads; sp.group = G; sp.q_dim = q_dim;
+    sp.tile_tokens = SHARED_TILE_ROWS / G;
+    sp.layer_block0 = (int)(2ull * layer * kv->n_pages * c.n_kv_heads);
+    sp.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
+    sp.part_o = p->part_o; sp.part_ml = p->part_ml;
+    sp.status = m->status_dev;
+    sp.seg_of_token = p->d<int>(p->o_seg); sp.seg_first = p->d<int>(p->o_seg_first);
+    sp.list_begin = p->d<int>(p->o_list_begin); sp.list = p->d<int>(p->o_list);
+    sp.out = out;
+    sp.n_items = p->n_items; sp.n_req = p->n_req; sp.n_tokens = p->T; sp.n_pages = (int)kv->n_pages;
+    sp.n_rows = p->n_rows; sp.n_list = p->n_list; sp.n_seg = p->n_seg;
+    // a tile: one 64-dim half of the G heads of a kv head for 128 / G tokens, i.e. rows (token, head) of 128 bytes
+    CUtensorMap tm;
+    cuuint64_t dims[4] = {64, c.head_dim / 64, c.n_q_heads, (cuuint64_t)p->T};
+    cuuint64_t strides[3] = {128, (cuuint64_t)c.head_dim * 2, (cuuint64_t)q_dim * 2};
+    cuuint32_t box[4] = {64, 1, G, (cuuint32_t)sp.tile_tokens}, estr[4] = {1, 1, 1, 1};
+    if (g_encode(&tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<op16*>(q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return SYN_E_CUDA;
+    const bool wide = c.head_dim == 128;
+    const int rows = p->T * (int)c.n_q_heads;
+    {
+        ProfScope prof(m, 2, st);
+        if ((wide ? launch_pdl(attn_shared_kernel<128>, dim3(p->n_cta), dim3(SHR_THREADS), SharedSmem<128>::TOTAL, st, tm, kv->tm_kv5, sp)
+                  : launch_pdl(attn_shared_kernel<64>, dim3(p->n_cta), dim3(SHR_THREADS), SharedSmem<64>::TOTAL, st, tm, kv->tm_kv5, sp)) != cudaSuccess)
+            return SYN_E_CUDA;
+    }
+    ProfScope prof(m, 3, st);
+    if ((wide ? launch_pdl(shared_merge_kernel<128>, dim3((rows + 3) / 4), dim3(128), 0, st, sp, rows)
+              : launch_pdl(shared_merge_kernel<64>, dim3((rows + 3) / 4), dim3(128), 0, st, sp, rows)) != cudaSuccess)
+        return SYN_E_CUDA;
+    return SYN_OK;
+}
+
 static int launch_attention(syn_model* m, syn_kv* kv, const syn_plan* p, uint32_t layer, const CUtensorMap& tmQ,
                             op16* out, cudaStream_t st) {
+    if (p->attn == ATTN_SHARED) return launch_shared(m, kv, p, layer, m->q, out, st);
     AttnParams ap;
     attn_params(ap, m, kv, p, layer, out, m->part_o, m->part_ml, m->group_count);
     if (p->attn == ATTN_THIN && 2 * p->n_parts > p->n_items) {
@@ -2308,7 +2462,7 @@ extern "C" int syn_debug_set_schedule(int32_t which) {
 }
 
 extern "C" int syn_debug_set_attention(int32_t which) {
-    if (which < 0 || which > 3) return SYN_E_INVALID_ARG;
+    if (which < 0 || which > 4) return SYN_E_INVALID_ARG;
     g_attention = which;
     return SYN_OK;
 }
@@ -2328,8 +2482,12 @@ static int syn_op_attention_impl(syn_model* m, syn_kv* kv, const syn_plan* p, ui
         return SYN_E_INVALID_ARG;
     const syn_model_desc& c = m->desc;
     const int q_dim = c.n_q_heads * c.head_dim;
-    if (p->T > m->t_cap || p->n_parts > m->part_cap) return SYN_E_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    if (p->attn == ATTN_SHARED) {   // reads the caller's q where it is
+        if (((uintptr_t)q & 15) || ((uintptr_t)out & 7)) return SYN_E_INVALID_ARG;
+        return launch_shared(m, kv, p, layer, (const op16*)q, (op16*)out, st);
+    }
+    if (p->T > m->t_cap || p->n_parts > m->part_cap) return SYN_E_INVALID_ARG;
     // the Q tensor map is bound to the workspace buffer: stage the caller's q there
     CU_OK(cudaMemcpyAsync(m->q, q, (size_t)p->T * q_dim * 2, cudaMemcpyDeviceToDevice, st));
     return launch_attention(m, kv, p, layer, m->tm_q, (op16*)out, st);
@@ -2377,6 +2535,7 @@ static int syn_op_attention_static_impl(syn_model* m, syn_kv* kv, const syn_plan
                                        void* out, void* cuda_stream) {
     if (!m || !kv || !p || kv->model != m || !plan_matches(p, kv) || !q || !out || layer >= m->desc.n_layers)
         return SYN_E_INVALID_ARG;
+    if (p->attn == ATTN_SHARED) return syn_op_attention_impl(m, kv, p, layer, q, out, cuda_stream);   // its partials are the plan's
     const syn_model_desc& c = m->desc;
     const int q_dim = c.n_q_heads * c.head_dim;
     if (p->T > m->t_cap) return SYN_E_INVALID_ARG;
@@ -2634,7 +2793,15 @@ extern "C" int syn_plan_work_host(const syn_model_desc* desc, uint32_t n_pages, 
 }
 
 extern "C" int syn_plan_create(syn_model* m, syn_kv* kv, int32_t n_req, const int32_t* chunk_tokens, const int32_t* chunk_offsets, const int32_t* page_tables, int32_t max_pages, const int32_t* ctx_lens, const int32_t* n_uncached, syn_plan** out) {
-    SYN_GUARD(syn_plan_create_impl(m, kv, n_req, chunk_tokens, chunk_offsets, page_tables, max_pages, ctx_lens, n_uncached, out));
+    SYN_GUARD(syn_plan_create_impl(m, kv, n_req, chunk_tokens, chunk_offsets, page_tables, max_pages, ctx_lens, n_uncached, false, out));
+}
+
+extern "C" int syn_plan_create_shared(syn_model* m, syn_kv* kv, int32_t n_req, const int32_t* chunk_tokens, const int32_t* chunk_offsets, const int32_t* page_tables, int32_t max_pages, const int32_t* ctx_lens, const int32_t* n_uncached, syn_plan** out) {
+    SYN_GUARD(syn_plan_create_impl(m, kv, n_req, chunk_tokens, chunk_offsets, page_tables, max_pages, ctx_lens, n_uncached, true, out));
+}
+
+extern "C" int syn_plan_shared_host(const syn_model_desc* desc, uint32_t n_pages, uint32_t page_size, int32_t n_sm, int32_t n_req, const int32_t* chunk_tokens, const int32_t* chunk_offsets, const int32_t* page_tables, int32_t max_pages, const int32_t* ctx_lens, const int32_t* n_uncached, int32_t* items, int32_t items_cap, int32_t* n_items, int32_t* cta_begin, int32_t* n_cta, int32_t* parts, int32_t parts_cap, int32_t* n_parts, int32_t* taken, syn_step_stats* stats) {
+    SYN_GUARD(syn_plan_shared_host_impl(desc, n_pages, page_size, n_sm, n_req, chunk_tokens, chunk_offsets, page_tables, max_pages, ctx_lens, n_uncached, items, items_cap, n_items, cta_begin, n_cta, parts, parts_cap, n_parts, taken, stats));
 }
 
 extern "C" int syn_verify_run(syn_model* m, syn_kv* kv, const syn_plan* p, int32_t* accept_len_dev, int32_t* correction_dev, int32_t* top1_dev, float* logits_out, void* cuda_stream) {
