@@ -14,8 +14,8 @@
 // cores work for the other.  With one tile the groups take alternate stages, as in attention2.cuh, and leave separate partials.
 // What bounds it: with two tiles the exponentials (16 a cycle and SM, as many cycles as the products take at full rate) and the
 // products in turn; with one tile the keys' bytes.
-// Warp roles: warp 3 streams pages and Q tiles (K and V have rings of their own), one thread of warp 2 issues every MMA, warps 4..7
-// and 8..11 are the softmax groups.  tcgen05 operations of one thread complete in order, so Q K^T of a group's next stage may
+// Warp roles: warp 3 streams pages and Q tiles (K and V have rings of their own), one thread of warp 1 and one of warp 2 issue the
+// MMAs of a group each, warps 4..7 and 8..11 are the softmax groups.  tcgen05 operations of one thread complete in order, so Q K^T of a group's next stage may
 // follow P V of its last in the same columns, and the commit behind it tells that both are done.  The maximum that P is relative to
 // is raised only when a stage exceeds it by 2^8; P is scaled by 2^7 besides (at most 2^15 in half precision, so that weights down to
 // 2^-21 of the largest keep all their bits).  Every wait is bounded.
@@ -29,7 +29,7 @@ constexpr int SHR_THREADS = 384;
 constexpr int SHR_PAGES = SHARED_STAGE / 16;
 constexpr int SHR_SOFTMAX_REGS = 208, SHR_OTHER_REGS = 88;
 static_assert(8 * SHR_SOFTMAX_REGS + 4 * SHR_OTHER_REGS <= 12 * ATT_LAUNCH_REGS, "the increase must fit in what the others give back");
-constexpr int SHR_PRODUCER_WARP = 3, SHR_MMA_WARP = 2;
+constexpr int SHR_PRODUCER_WARP = 3, SHR_MMA_WARP0 = 1, SHR_ALLOC_WARP = 0;
 constexpr float SHR_P_SCALE_LOG2 = 7.0f;
 
 struct SharedParams {
@@ -90,10 +90,12 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     uint8_t* qbuf = smem;                               // two slots
     uint8_t* kring = qbuf + 2 * SM::Q_BYTES;
     uint8_t* vring = kring + KS * SM::K_BYTES;
-    uint64_t* k_full = reinterpret_cast<uint64_t*>(vring + VS * SM::K_BYTES);
-    uint64_t* k_empty = k_full + KS;     // every score of the stage is complete
-    uint64_t* v_full = k_empty + KS;
-    uint64_t* v_empty = v_full + VS;     // every P V of the stage is complete
+    // A wait on a phase's parity must not be two phases off: whoever waits on a barrier has to see every one of its phases.  So
+    // a slot has three "full" barriers, for stages of group 0, of group 1 and of both, and the Q slots are watched by both issuers.
+    uint64_t* k_full = reinterpret_cast<uint64_t*>(vring + VS * SM::K_BYTES);   // [who][slot]
+    uint64_t* k_empty = k_full + 3 * KS; // every score of the stage is complete
+    uint64_t* v_full = k_empty + KS;     // [who][slot]
+    uint64_t* v_empty = v_full + 3 * VS; // every P V of the stage is complete
     uint64_t* q_full = v_empty + VS;     // [slot]
     uint64_t* q_empty = q_full + 2;      // [slot] the last Q K^T that reads it is complete
     uint64_t* s_full = q_empty + 2;      // [group] scores of a stage (and every P V before) are complete
@@ -101,7 +103,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     uint64_t* o_full = p_full + 2;       // [group] the item's last P V is complete
     uint64_t* o_empty = o_full + 2;      // [group] its warps have read O
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_empty + 2);
-    static_assert((2 * KS + 2 * VS + 12) * 8 + 4 <= 512, "barrier area");
+    static_assert((4 * KS + 4 * VS + 12) * 8 + 4 <= 512, "barrier area");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int it_begin = p.cta_begin[blockIdx.x], it_end = p.cta_begin[blockIdx.x + 1];
@@ -111,11 +113,13 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     if (threadIdx.x == 0) {
         tma_prefetch_desc(&tmQ);
         tma_prefetch_desc(&tmKV);
-        for (int s = 0; s < KS; ++s) { mbar_init(&k_full[s], 1); mbar_init(&k_empty[s], 1); }
-        for (int s = 0; s < VS; ++s) { mbar_init(&v_full[s], 1); mbar_init(&v_empty[s], 1); }
+        for (int s = 0; s < 3 * KS; ++s) mbar_init(&k_full[s], 1);
+        for (int s = 0; s < 3 * VS; ++s) mbar_init(&v_full[s], 1);
+        for (int s = 0; s < KS; ++s) mbar_init(&k_empty[s], 2);
+        for (int s = 0; s < VS; ++s) mbar_init(&v_empty[s], 2);
         for (int s = 0; s < 2; ++s) {
             mbar_init(&q_full[s], 1);
-            mbar_init(&q_empty[s], 1);
+            mbar_init(&q_empty[s], 2);
             mbar_init(&s_full[s], 1);
             mbar_init(&p_full[s], 4);
             mbar_init(&o_full[s], 1);
@@ -124,7 +128,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         mbar_fence_init();
         if (!list_ok) atomicExch(p.status, 2);
     }
-    if (warp == SHR_MMA_WARP) {
+    if (warp == SHR_ALLOC_WARP) {
         tmem_alloc(tmem_slot, SM::TMEM_COLS);
         tmem_relinquish();
     }
@@ -179,7 +183,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll
                     for (int v = 0; v < 2; ++v) {
                         const uint32_t n = v ? VS : KS, s = st % n;
-                        uint64_t* full = v ? v_full : k_full;
+                        uint64_t* full = (v ? v_full : k_full) + (item.tiles == 2 ? 2 : k & 1) * n;
                         if (lane == 0) {
                             if (st >= n) ok = mbar_wait(&(v ? v_empty : k_empty)[s], ((st / n) - 1) & 1u, p.status);
                             if (ok) mbar_expect_tx(&full[s], (uint32_t)npg * SM::BOX_BYTES);
@@ -192,108 +196,75 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                     if (!ok) break;
                 }
             }
-        } else if (warp == SHR_MMA_WARP && elect_one()) {
-            // -------------------------------------------------------- MMA issuer
-            // Each group's stages go Q K^T, P V, Q K^T, ... ; the thread issues whatever is ready, k-steps of both groups in
-            // turn when both are (an MMA into the accumulator of the one before it waits for it, attention2.cuh).
-            constexpr uint32_t QK_STEPS = HD / 16;
-            const uint32_t idesc_pv = umma_idesc_f16_bmn(128, HD);
+        } else if (warp >= SHR_MMA_WARP0 && warp < SHR_MMA_WARP0 + 2 && elect_one()) {
+            // -------------------------------------------------------- MMA issuers, one a group
+            // A group's stages go Q K^T, P V, Q K^T, ...; the two issuers' products interleave, which hides that an MMA into the
+            // accumulator of the one before it waits for it (attention2.cuh).  The barriers of a slot count two commits: both
+            // issuers' where both use it, twice the one's where it is the only one.
+            const int w = warp - SHR_MMA_WARP0;
+            const uint32_t idesc_pv = umma_idesc_f16_bmn(128, HD), idesc_qk = umma_idesc_f16(128, SHARED_STAGE);
+            const uint32_t s_tmem = tmem_base + 256 + w * 128, o_tmem = tmem_base + w * 128;
             uint32_t st = 0, qs = 0;         // stage and Q slot of the item's first
-            uint32_t use[2] = {0, 0};        // stages of each group in the items before
-            uint32_t o_use[2] = {0, 0};      // items of each group before
+            uint32_t use = 0, o_use = 0;     // stages and items of the group so far
+            uint32_t k_own = 0, k_both = 0, v_own = 0, v_both = 0;   // bit s: parity of the next phase of slot s
             bool ok = true;
             for (int it = it_begin; list_ok && it < it_end && ok; ++it) {
                 const SharedItem item = p.items[it];
                 if (!shared_item_ok(item, p)) break;
                 const bool two = item.tiles == 2;
-                const uint32_t n_st = (uint32_t)(item.kv_end - item.kv_begin + SHARED_STAGE - 1) / SHARED_STAGE;
-                const uint32_t n[2] = {two ? n_st : (n_st + 1) / 2, two ? n_st : n_st / 2};
-                uint32_t nq[2] = {0, 0}, np[2] = {0, 0};   // Q K^T and P V issued
-                auto stage_of = [&](int w, uint32_t i) { return two ? i : 2 * i + w; };
-                auto pages_of = [&](uint32_t k) { return (uint32_t)min(SHR_PAGES, (item.kv_end - item.kv_begin - (int)k * SHARED_STAGE + 15) >> 4); };
-                long long t0 = 0;
-                uint32_t idle = 0;
-                while (np[0] < n[0] || np[1] < n[1]) {
-                    int op[2];               // 1: Q K^T, 2: P V
-                    uint32_t steps[2] = {0, 0}, d[2], a_tmem[2], idesc[2];
-                    uint64_t a[2], b[2];
-                    uint32_t at[2];
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        op[w] = 0;
-                        if (nq[w] == np[w] && nq[w] < n[w]) {
-                            const uint32_t s = st + stage_of(w, nq[w]), q = qs + (two ? w : 0);
-                            if (mbar_test(&k_full[s % KS], (s / KS) & 1u) && mbar_test(&q_full[q & 1u], (q >> 1) & 1u)) {
-                                op[w] = 1;
-                                steps[w] = QK_STEPS;
-                                d[w] = tmem_base + 256 + w * 128;
-                                a[w] = umma_desc_k128(smem_u32(qbuf + (q & 1u) * SM::Q_BYTES));
-                                b[w] = umma_desc_k128s(smem_u32(kring + (s % KS) * SM::K_BYTES), SM::GROUP_BYTES);
-                                idesc[w] = umma_idesc_f16(128, 16 * pages_of(s - st));
-                                at[w] = s - st;
-                            }
-                        } else if (np[w] < nq[w]) {
-                            const uint32_t s = st + stage_of(w, np[w]), u = use[w] + np[w];
-                            if (mbar_test(&p_full[w], u & 1u) && mbar_test(&v_full[s % VS], (s / VS) & 1u) &&
-                                (np[w] > 0 || o_use[w] == 0 || mbar_test(&o_empty[w], (o_use[w] - 1) & 1u))) {
-                                op[w] = 2;
-                                steps[w] = pages_of(s - st);
-                                d[w] = tmem_base + w * 128;
-                                a_tmem[w] = tmem_base + 256 + w * 128;
-                                b[w] = umma_desc_mn128(smem_u32(vring + (s % VS) * SM::K_BYTES), 1024, SM::GROUP_BYTES);
-                                idesc[w] = idesc_pv;
-                                at[w] = s - st;
-                            }
-                        }
-                    }
-                    if (!op[0] && !op[1]) {
-                        if ((++idle & 0x3FFu) == 0) {
-                            const long long now = clock64();
-                            if (t0 == 0) t0 = now;
-                            else if (now - t0 > SYN_SPIN_LIMIT_CYCLES) {
-                                atomicExch(p.status, 1);
-                                ok = false;
-                                break;
-                            }
-                        }
-                        continue;
-                    }
-                    idle = 0;
-                    t0 = 0;
+                const int who = two ? 2 : w, keys = item.kv_end - item.kv_begin;
+                const uint32_t n_st = (uint32_t)(keys + SHARED_STAGE - 1) / SHARED_STAGE, step = two ? 1 : 2;
+                const uint32_t q_addr = smem_u32(qbuf + ((qs + (two ? w : 0)) & 1u) * SM::Q_BYTES);
+                for (uint32_t q = qs; q < qs + item.tiles && ok; ++q) ok = mbar_wait(&q_full[q & 1u], (q >> 1) & 1u, p.status);
+                if (!ok) break;
+                if (!two && (uint32_t)w >= n_st) mbar_arrive(&q_empty[qs & 1u]);   // nothing here for the second group
+                uint32_t kb = two ? k_both : k_own, vb = two ? v_both : v_own;
+                for (uint32_t k = two ? 0 : w; k < n_st; k += step) {
+                    const uint32_t s = st + k, ks = s % KS, vs = s % VS;
+                    const uint32_t pages = (uint32_t)min(SHR_PAGES, (keys - (int)k * SHARED_STAGE + 15) >> 4);
+                    const bool first = k < step, last = k + step >= n_st;
+                    ok = mbar_wait(&k_full[who * KS + ks], (kb >> ks) & 1u, p.status);
+                    if (!ok) break;
+                    kb ^= 1u << ks;
                     tc_fence_after();
+                    {
+                        const uint64_t a = umma_desc_k128(q_addr), b = umma_desc_k128s(smem_u32(kring + ks * SM::K_BYTES), SM::GROUP_BYTES);
+                        const uint32_t idesc = pages == SHR_PAGES ? idesc_qk : umma_idesc_f16(128, 16 * pages);
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) {
+                        for (uint32_t i = 0; i < HD / 16; ++i)   // step i: 16 dims, of the second half from step 4 on
+                            umma_bf16(s_tmem, a + (i >> 2) * (SM::Q_HALF >> 4) + 2 * (i & 3), b + (i >> 2) * (1024 >> 4) + 2 * (i & 3), idesc, i != 0);
+                    }
+                    umma_commit(&s_full[w]);
+                    umma_commit(&k_empty[ks]);
+                    if (!two) umma_commit(&k_empty[ks]);
+                    if (last)
+                        for (uint32_t q = qs; q < qs + item.tiles; ++q) umma_commit(&q_empty[q & 1u]);
+                    ok = mbar_wait(&p_full[w], use & 1u, p.status);
+                    if (ok) ok = mbar_wait(&v_full[who * VS + vs], (vb >> vs) & 1u, p.status);
+                    if (ok && first && o_use > 0) ok = mbar_wait(&o_empty[w], (o_use - 1) & 1u, p.status);
+                    if (!ok) break;
+                    vb ^= 1u << vs;
+                    tc_fence_after();
+                    {
+                        const uint64_t b = umma_desc_mn128(smem_u32(vring + vs * SM::K_BYTES), 1024, SM::GROUP_BYTES);
+                        if (pages == SHR_PAGES) {
 #pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            if (i >= steps[w]) continue;
-                            if (op[w] == 1)   // step i: 16 dims, of the second half from step 4 on
-                                umma_bf16(d[w], a[w] + (i >> 2) * (SM::Q_HALF >> 4) + 2 * (i & 3), b[w] + (i >> 2) * (1024 >> 4) + 2 * (i & 3), idesc[w], i != 0);
-                            else              // step i: the 16 keys of a page; the item's first P V starts its O afresh
-                                umma_f16_ta(d[w], a_tmem[w] + 8 * i, b[w] + i * (SM::BOX_BYTES >> 4), idesc[w], np[w] != 0 || i != 0);
+                            for (uint32_t i = 0; i < SHR_PAGES; ++i)   // step i: the 16 keys of a page; the item's first P V starts its O afresh
+                                umma_f16_ta(o_tmem, s_tmem + 8 * i, b + i * (SM::BOX_BYTES >> 4), idesc_pv, !first || i != 0);
+                        } else {
+                            for (uint32_t i = 0; i < pages; ++i) umma_f16_ta(o_tmem, s_tmem + 8 * i, b + i * (SM::BOX_BYTES >> 4), idesc_pv, !first || i != 0);
                         }
                     }
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const uint32_t s = st + at[w];
-                        if (op[w] == 1) {
-                            ++nq[w];
-                            umma_commit(&s_full[w]);
-                            if (!two || nq[w ^ 1] >= nq[w]) umma_commit(&k_empty[s % KS]);   // the other tile has had this stage's K
-                            if (two ? nq[w] == n[w] : nq[0] == n[0] && nq[1] == n[1]) umma_commit(&q_empty[(qs + (two ? w : 0)) & 1u]);
-                        } else if (op[w] == 2) {
-                            ++np[w];
-                            if (!two || np[w ^ 1] >= np[w]) umma_commit(&v_empty[s % VS]);
-                            if (np[w] == n[w]) umma_commit(&o_full[w]);
-                        }
-                    }
+                    umma_commit(&v_empty[vs]);
+                    if (!two) umma_commit(&v_empty[vs]);
+                    if (last) umma_commit(&o_full[w]);
+                    ++use;
                 }
+                (two ? k_both : k_own) = kb;
+                (two ? v_both : v_own) = vb;
                 st += n_st;
                 qs += item.tiles;
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    use[w] += n[w];
-                    o_use[w] += n[w] > 0;
-                }
+                o_use += two || (uint32_t)w < n_st;
             }
         }
         __syncwarp();
@@ -305,6 +276,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const uint32_t t_lane = tmem_base + ((uint32_t)(wq * 32) << 16);
         const uint32_t o_col = (uint32_t)wg * 128, s_col = 256 + (uint32_t)wg * 128;
         uint32_t st = 0, use = 0, o_use = 0;
+        uint32_t v_own = 0, v_both = 0;   // as the issuer's
         bool ok = true;   // uniform over the warp: the tensor-memory loads and stores are warp-wide
         auto wait_all = [&](uint64_t* bar, uint32_t parity) {
             const bool r = mbar_wait(bar, parity, p.status);
@@ -328,6 +300,8 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             for (int k = 0; k < n_st; ++k) {
                 if (!two && (k & 1) != wg) continue;
                 const int kv0 = item.kv_begin + k * SHARED_STAGE;
+                const uint32_t vs = (st + k) % VS, v_parity = ((two ? v_both : v_own) >> vs) & 1u;
+                (two ? v_both : v_own) ^= 1u << vs;
                 if (ok) ok = wait_all(&s_full[wg], use & 1u);
                 ++use;
                 if (wlive && ok) {
@@ -345,12 +319,14 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                             for (int i = 0; i < 32; ++i)
                                 if (32 * c + i >= nvalid) s[c][i] = 0xFF800000u;   // -inf
                     }
-                    float mx = -INFINITY;
+                    float mc[4];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < 4; ++c) {
+                        mc[c] = __uint_as_float(s[c][0]);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(s[c][i]));
-                    const float ms = mx * p.scale_log2;
+                        for (int i = 1; i < 32; ++i) mc[c] = fmaxf(mc[c], __uint_as_float(s[c][i]));
+                    }
+                    const float ms = fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3])) * p.scale_log2;
                     if (mine == 0) {
                         m_used = live ? ms : 0.f;
                     } else {
@@ -393,8 +369,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 // Rows of the last page behind the item's keys: a weight of zero takes whatever is stale there out, unless that is no
                 // number.  Every group that uses the stage clears them before its P V can start.
                 if ((item.kv_end & 15) && k == n_st - 1 && ok) {
-                    const uint32_t vs = (st + k) % VS;
-                    ok = wait_all(&v_full[vs], ((st + k) / VS) & 1u);
+                    ok = wait_all(&v_full[(two ? 2 : wg) * VS + vs], v_parity);
                     uint8_t* box = vring + vs * SM::K_BYTES + ((item.kv_end - 1 - kv0) >> 4) * SM::BOX_BYTES;
                     const int r0 = item.kv_end & 15;
                     for (int c = row; ok && c < (16 - r0) * HALVES * 8; c += 128) {
@@ -436,7 +411,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     // ---------------------------------------------------------------- teardown
     tc_fence_before();
     __syncthreads();
-    if (warp == SHR_MMA_WARP) {
+    if (warp == SHR_ALLOC_WARP) {
         tc_fence_after();
         tmem_dealloc(tmem_base, SM::TMEM_COLS);
     }
