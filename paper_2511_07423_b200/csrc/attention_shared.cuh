@@ -14,8 +14,8 @@
 // cores work for the other.  With one tile the groups take alternate stages, as in attention2.cuh, and leave separate partials.
 // What bounds it: with two tiles the exponentials (16 a cycle and SM, as many cycles as the products take at full rate) and the
 // products in turn; with one tile the keys' bytes.
-// Warp roles: warp 3 streams pages and Q tiles (K and V have rings of their own), one thread of warp 1 and one of warp 2 issue the
-// MMAs of a group each, warps 4..7 and 8..11 are the softmax groups.  tcgen05 operations of one thread complete in order, so Q K^T of a group's next stage may
+// Warp roles: warp 3 streams pages and Q tiles (K and V have rings of their own), one thread of warp 2 issues every
+// MMA, warps 4..7 and 8..11 are the softmax groups.  tcgen05 operations of one thread complete in order, so Q K^T of a group's next stage may
 // follow P V of its last in the same columns, and the commit behind it tells that both are done.  The maximum that P is relative to
 // is raised only when a stage exceeds it by 2^8; P is scaled by 2^7 besides (at most 2^15 in half precision, so that weights down to
 // 2^-21 of the largest keep all their bits).  Every wait is bounded.
@@ -29,7 +29,7 @@ constexpr int SHR_THREADS = 384;
 constexpr int SHR_PAGES = SHARED_STAGE / 16;
 constexpr int SHR_SOFTMAX_REGS = 208, SHR_OTHER_REGS = 88;
 static_assert(8 * SHR_SOFTMAX_REGS + 4 * SHR_OTHER_REGS <= 12 * ATT_LAUNCH_REGS, "the increase must fit in what the others give back");
-constexpr int SHR_PRODUCER_WARP = 3, SHR_MMA_WARP0 = 1, SHR_ALLOC_WARP = 0;
+constexpr int SHR_PRODUCER_WARP = 3, SHR_MMA_WARP = 2;
 constexpr float SHR_P_SCALE_LOG2 = 7.0f;
 
 struct SharedParams {
@@ -90,12 +90,11 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     uint8_t* qbuf = smem;                               // two slots
     uint8_t* kring = qbuf + 2 * SM::Q_BYTES;
     uint8_t* vring = kring + KS * SM::K_BYTES;
-    // A wait on a phase's parity must not be two phases off: whoever waits on a barrier has to see every one of its phases.  So
-    // a slot has three "full" barriers, for stages of group 0, of group 1 and of both, and the Q slots are watched by both issuers.
-    uint64_t* k_full = reinterpret_cast<uint64_t*>(vring + VS * SM::K_BYTES);   // [who][slot]
-    uint64_t* k_empty = k_full + 3 * KS; // every score of the stage is complete
-    uint64_t* v_full = k_empty + KS;     // [who][slot]
-    uint64_t* v_empty = v_full + 3 * VS; // every P V of the stage is complete
+    // (A wait on a phase's parity must not be two phases off: whoever waits on a barrier has to see every one of its phases.)
+    uint64_t* k_full = reinterpret_cast<uint64_t*>(vring + VS * SM::K_BYTES);
+    uint64_t* k_empty = k_full + KS;     // every score of the stage is complete
+    uint64_t* v_full = k_empty + KS;
+    uint64_t* v_empty = v_full + VS;     // every P V of the stage is complete
     uint64_t* q_full = v_empty + VS;     // [slot]
     uint64_t* q_empty = q_full + 2;      // [slot] the last Q K^T that reads it is complete
     uint64_t* s_full = q_empty + 2;      // [group] scores of a stage (and every P V before) are complete
@@ -103,7 +102,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     uint64_t* o_full = p_full + 2;       // [group] the item's last P V is complete
     uint64_t* o_empty = o_full + 2;      // [group] its warps have read O
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_empty + 2);
-    static_assert((4 * KS + 4 * VS + 12) * 8 + 4 <= 512, "barrier area");
+    static_assert((2 * KS + 2 * VS + 12) * 8 + 4 <= 512, "barrier area");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int it_begin = p.cta_begin[blockIdx.x], it_end = p.cta_begin[blockIdx.x + 1];
@@ -113,13 +112,11 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     if (threadIdx.x == 0) {
         tma_prefetch_desc(&tmQ);
         tma_prefetch_desc(&tmKV);
-        for (int s = 0; s < 3 * KS; ++s) mbar_init(&k_full[s], 1);
-        for (int s = 0; s < 3 * VS; ++s) mbar_init(&v_full[s], 1);
-        for (int s = 0; s < KS; ++s) mbar_init(&k_empty[s], 2);
-        for (int s = 0; s < VS; ++s) mbar_init(&v_empty[s], 2);
+        for (int s = 0; s < KS; ++s) { mbar_init(&k_full[s], 1); mbar_init(&k_empty[s], 1); }
+        for (int s = 0; s < VS; ++s) { mbar_init(&v_full[s], 1); mbar_init(&v_empty[s], 1); }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&q_full[s], 1);
-            mbar_init(&q_empty[s], 2);
+            mbar_init(&q_empty[s], 1);
             mbar_init(&s_full[s], 1);
             mbar_init(&p_full[s], 4);
             mbar_init(&o_full[s], 1);
@@ -128,7 +125,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         mbar_fence_init();
         if (!list_ok) atomicExch(p.status, 2);
     }
-    if (warp == SHR_ALLOC_WARP) {
+    if (warp == SHR_MMA_WARP) {
         tmem_alloc(tmem_slot, SM::TMEM_COLS);
         tmem_relinquish();
     }
@@ -183,7 +180,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll
                     for (int v = 0; v < 2; ++v) {
                         const uint32_t n = v ? VS : KS, s = st % n;
-                        uint64_t* full = (v ? v_full : k_full) + (item.tiles == 2 ? 2 : k & 1) * n;
+                        uint64_t* full = v ? v_full : k_full;
                         if (lane == 0) {
                             if (st >= n) ok = mbar_wait(&(v ? v_empty : k_empty)[s], ((st / n) - 1) & 1u, p.status);
                             if (ok) mbar_expect_tx(&full[s], (uint32_t)npg * SM::BOX_BYTES);
@@ -196,76 +193,84 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                     if (!ok) break;
                 }
             }
-        } else if (warp >= SHR_MMA_WARP0 && warp < SHR_MMA_WARP0 + 2 && elect_one()) {
-            // -------------------------------------------------------- MMA issuers, one a group
-            // A group's stages go Q K^T, P V, Q K^T, ...; the two issuers' products interleave, which hides that an MMA into the
-            // accumulator of the one before it waits for it (attention2.cuh).  The barriers of a slot count two commits: both
-            // issuers' where both use it, twice the one's where it is the only one.
-            const int w = warp - SHR_MMA_WARP0;
+        } else if (warp == SHR_MMA_WARP && elect_one()) {
+            // -------------------------------------------------------- MMA issuer
+            // The groups take turns: P V of a group's stage, Q K^T of its next, then the other group's.  In this order, which
+            // the tensor cores keep, one group's scores are ready half a stage's time before the other's, so that one computes
+            // exponentials while the products of the other run (issued by whichever is ready, the two fall into step: both
+            // compute, then both wait; 5 300 cycles a stage instead of SHR_STAGE2).  A group's P V waits for its turn in the next item.
             const uint32_t idesc_pv = umma_idesc_f16_bmn(128, HD), idesc_qk = umma_idesc_f16(128, SHARED_STAGE);
-            const uint32_t s_tmem = tmem_base + 256 + w * 128, o_tmem = tmem_base + w * 128;
-            uint32_t st = 0, qs = 0;         // stage and Q slot of the item's first
-            uint32_t use = 0, o_use = 0;     // stages and items of the group so far
-            uint32_t k_own = 0, k_both = 0, v_own = 0, v_both = 0;   // bit s: parity of the next phase of slot s
+            struct Pending { uint32_t pages, vs, v_parity; bool any, first, last, wait_v, free_v; };   // a group's P V to come
+            Pending pend[2];
+            pend[0].any = pend[1].any = false;
+            uint32_t use[2] = {0, 0}, o_use[2] = {0, 0};   // P V's of each group so far, and items among them
+            uint32_t st = 0, qs = 0;                       // stage and Q slot of the item's first
             bool ok = true;
+            auto pv = [&](int w) {
+                const Pending& n = pend[w];
+                pend[w].any = false;
+                ok = mbar_wait(&p_full[w], use[w] & 1u, p.status);
+                if (ok && n.wait_v) ok = mbar_wait(&v_full[n.vs], n.v_parity, p.status);
+                if (ok && n.first && o_use[w] > 0) ok = mbar_wait(&o_empty[w], (o_use[w] - 1) & 1u, p.status);
+                if (!ok) return;
+                tc_fence_after();
+                const uint32_t s_tmem = tmem_base + 256 + w * 128, o_tmem = tmem_base + w * 128;
+                const uint64_t b = umma_desc_mn128(smem_u32(vring + n.vs * SM::K_BYTES), 1024, SM::GROUP_BYTES);
+                if (n.pages == SHR_PAGES) {
+#pragma unroll
+                    for (uint32_t i = 0; i < SHR_PAGES; ++i)   // step i: the 16 keys of a page; an item's first P V starts its O afresh
+                        umma_f16_ta(o_tmem, s_tmem + 8 * i, b + i * (SM::BOX_BYTES >> 4), idesc_pv, !n.first || i != 0);
+                } else {
+                    for (uint32_t i = 0; i < n.pages; ++i) umma_f16_ta(o_tmem, s_tmem + 8 * i, b + i * (SM::BOX_BYTES >> 4), idesc_pv, !n.first || i != 0);
+                }
+                if (n.free_v) umma_commit(&v_empty[n.vs]);
+                if (n.last) {
+                    umma_commit(&o_full[w]);
+                    ++o_use[w];
+                }
+                ++use[w];
+            };
             for (int it = it_begin; list_ok && it < it_end && ok; ++it) {
                 const SharedItem item = p.items[it];
                 if (!shared_item_ok(item, p)) break;
                 const bool two = item.tiles == 2;
-                const int who = two ? 2 : w, keys = item.kv_end - item.kv_begin;
+                const int keys = item.kv_end - item.kv_begin;
                 const uint32_t n_st = (uint32_t)(keys + SHARED_STAGE - 1) / SHARED_STAGE, step = two ? 1 : 2;
-                const uint32_t q_addr = smem_u32(qbuf + ((qs + (two ? w : 0)) & 1u) * SM::Q_BYTES);
                 for (uint32_t q = qs; q < qs + item.tiles && ok; ++q) ok = mbar_wait(&q_full[q & 1u], (q >> 1) & 1u, p.status);
-                if (!ok) break;
-                if (!two && (uint32_t)w >= n_st) mbar_arrive(&q_empty[qs & 1u]);   // nothing here for the second group
-                uint32_t kb = two ? k_both : k_own, vb = two ? v_both : v_own;
-                for (uint32_t k = two ? 0 : w; k < n_st; k += step) {
-                    const uint32_t s = st + k, ks = s % KS, vs = s % VS;
-                    const uint32_t pages = (uint32_t)min(SHR_PAGES, (keys - (int)k * SHARED_STAGE + 15) >> 4);
-                    const bool first = k < step, last = k + step >= n_st;
-                    ok = mbar_wait(&k_full[who * KS + ks], (kb >> ks) & 1u, p.status);
-                    if (!ok) break;
-                    kb ^= 1u << ks;
-                    tc_fence_after();
-                    {
-                        const uint64_t a = umma_desc_k128(q_addr), b = umma_desc_k128s(smem_u32(kring + ks * SM::K_BYTES), SM::GROUP_BYTES);
+                for (uint32_t k0 = 0; k0 < n_st && ok; k0 += step) {
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        const uint32_t k = two ? k0 : k0 + w;
+                        if (k >= n_st || !ok) continue;
+                        if (pend[w].any) pv(w);
+                        const uint32_t s = st + k, ks = s % KS;
+                        const uint32_t pages = (uint32_t)min(SHR_PAGES, (keys - (int)k * SHARED_STAGE + 15) >> 4);
+                        if (ok && (!two || w == 0)) ok = mbar_wait(&k_full[ks], (s / KS) & 1u, p.status);   // (seen by the other's turn)
+                        if (!ok) continue;
+                        tc_fence_after();
+                        const uint32_t s_tmem = tmem_base + 256 + w * 128;
+                        const uint64_t a = umma_desc_k128(smem_u32(qbuf + ((qs + (two ? w : 0)) & 1u) * SM::Q_BYTES));
+                        const uint64_t b = umma_desc_k128s(smem_u32(kring + ks * SM::K_BYTES), SM::GROUP_BYTES);
                         const uint32_t idesc = pages == SHR_PAGES ? idesc_qk : umma_idesc_f16(128, 16 * pages);
 #pragma unroll
                         for (uint32_t i = 0; i < HD / 16; ++i)   // step i: 16 dims, of the second half from step 4 on
                             umma_bf16(s_tmem, a + (i >> 2) * (SM::Q_HALF >> 4) + 2 * (i & 3), b + (i >> 2) * (1024 >> 4) + 2 * (i & 3), idesc, i != 0);
+                        umma_commit(&s_full[w]);
+                        const bool all = !two || w == 1;         // nobody else has the stage to come
+                        if (all) umma_commit(&k_empty[ks]);
+                        if (all && k == n_st - 1)
+                            for (uint32_t q = qs; q < qs + item.tiles; ++q) umma_commit(&q_empty[q & 1u]);
+                        pend[w] = Pending{pages, s % VS, (s / VS) & 1u, true, k < step, k + step >= n_st, !two || w == 0, all};
                     }
-                    umma_commit(&s_full[w]);
-                    umma_commit(&k_empty[ks]);
-                    if (!two) umma_commit(&k_empty[ks]);
-                    if (last)
-                        for (uint32_t q = qs; q < qs + item.tiles; ++q) umma_commit(&q_empty[q & 1u]);
-                    ok = mbar_wait(&p_full[w], use & 1u, p.status);
-                    if (ok) ok = mbar_wait(&v_full[who * VS + vs], (vb >> vs) & 1u, p.status);
-                    if (ok && first && o_use > 0) ok = mbar_wait(&o_empty[w], (o_use - 1) & 1u, p.status);
-                    if (!ok) break;
-                    vb ^= 1u << vs;
-                    tc_fence_after();
-                    {
-                        const uint64_t b = umma_desc_mn128(smem_u32(vring + vs * SM::K_BYTES), 1024, SM::GROUP_BYTES);
-                        if (pages == SHR_PAGES) {
-#pragma unroll
-                            for (uint32_t i = 0; i < SHR_PAGES; ++i)   // step i: the 16 keys of a page; the item's first P V starts its O afresh
-                                umma_f16_ta(o_tmem, s_tmem + 8 * i, b + i * (SM::BOX_BYTES >> 4), idesc_pv, !first || i != 0);
-                        } else {
-                            for (uint32_t i = 0; i < pages; ++i) umma_f16_ta(o_tmem, s_tmem + 8 * i, b + i * (SM::BOX_BYTES >> 4), idesc_pv, !first || i != 0);
-                        }
-                    }
-                    umma_commit(&v_empty[vs]);
-                    if (!two) umma_commit(&v_empty[vs]);
-                    if (last) umma_commit(&o_full[w]);
-                    ++use;
                 }
-                (two ? k_both : k_own) = kb;
-                (two ? v_both : v_own) = vb;
+                // an odd number of turns: the second group's P V is older than the first's, and its V slot is needed before its turn
+                // would come again (after any number of items of one stage)
+                if (ok && !two && (n_st & 1) && pend[1].any) pv(1);
                 st += n_st;
                 qs += item.tiles;
-                o_use += two || (uint32_t)w < n_st;
             }
+            for (int w = 0; w < 2; ++w)
+                if (ok && pend[w].any) pv(w);
         }
         __syncwarp();
     } else {
@@ -276,7 +281,6 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const uint32_t t_lane = tmem_base + ((uint32_t)(wq * 32) << 16);
         const uint32_t o_col = (uint32_t)wg * 128, s_col = 256 + (uint32_t)wg * 128;
         uint32_t st = 0, use = 0, o_use = 0;
-        uint32_t v_own = 0, v_both = 0;   // as the issuer's
         bool ok = true;   // uniform over the warp: the tensor-memory loads and stores are warp-wide
         auto wait_all = [&](uint64_t* bar, uint32_t parity) {
             const bool r = mbar_wait(bar, parity, p.status);
@@ -300,8 +304,6 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             for (int k = 0; k < n_st; ++k) {
                 if (!two && (k & 1) != wg) continue;
                 const int kv0 = item.kv_begin + k * SHARED_STAGE;
-                const uint32_t vs = (st + k) % VS, v_parity = ((two ? v_both : v_own) >> vs) & 1u;
-                (two ? v_both : v_own) ^= 1u << vs;
                 if (ok) ok = wait_all(&s_full[wg], use & 1u);
                 ++use;
                 if (wlive && ok) {
@@ -369,7 +371,9 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 // Rows of the last page behind the item's keys: a weight of zero takes whatever is stale there out, unless that is no
                 // number.  Every group that uses the stage clears them before its P V can start.
                 if ((item.kv_end & 15) && k == n_st - 1 && ok) {
-                    ok = wait_all(&v_full[(two ? 2 : wg) * VS + vs], v_parity);
+                    const uint32_t vs = (st + k) % VS;
+                    // (its phase before is over: the scores of this stage were issued behind the P V that used the slot)
+                    ok = wait_all(&v_full[vs], ((st + k) / VS) & 1u);
                     uint8_t* box = vring + vs * SM::K_BYTES + ((item.kv_end - 1 - kv0) >> 4) * SM::BOX_BYTES;
                     const int r0 = item.kv_end & 15;
                     for (int c = row; ok && c < (16 - r0) * HALVES * 8; c += 128) {
@@ -411,7 +415,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     // ---------------------------------------------------------------- teardown
     tc_fence_before();
     __syncthreads();
-    if (warp == SHR_ALLOC_WARP) {
+    if (warp == SHR_MMA_WARP) {
         tc_fence_after();
         tmem_dealloc(tmem_base, SM::TMEM_COLS);
     }
