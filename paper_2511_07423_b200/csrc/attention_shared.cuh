@@ -14,8 +14,8 @@
 // cores work for the other.  With one tile the groups take alternate stages, as in attention2.cuh, and leave separate partials.
 // What bounds it: with two tiles the exponentials (16 a cycle and SM, as many cycles as the products take at full rate) and the
 // products in turn; with one tile the keys' bytes.
-// Warp roles: warp 3 streams pages and Q tiles (K and V have rings of their own), one thread of warp 2 issues every
-// MMA, warps 4..7 and 8..11 are the softmax groups.  tcgen05 operations of one thread complete in order, so Q K^T of a group's next stage may
+// Warp roles: warp 3 streams pages and Q tiles (K and V have rings of their own), one thread of warp 1 and one of warp 2 issue the
+// MMAs of a group each, warps 4..7 and 8..11 are the softmax groups.  tcgen05 operations of one thread complete in order, so Q K^T of a group's next stage may
 // follow P V of its last in the same columns, and the commit behind it tells that both are done.  The maximum that P is relative to
 // is raised only when a stage exceeds it by 2^8; P is scaled by 2^7 besides (at most 2^15 in half precision, so that weights down to
 // 2^-21 of the largest keep all their bits).  Every wait is bounded.
@@ -25,11 +25,11 @@
 
 namespace syn {
 
-constexpr int SHR_THREADS = 384;
-constexpr int SHR_PAGES = SHARED_STAGE / 16;
+constexpr int SHR_THREADS = 384, SHR_BAR_BYTES = 768;
+constexpr int SHR_PAGES = SHARED_STAGE / 16, SHR_HALF = SHARED_STAGE / 2;
 constexpr int SHR_SOFTMAX_REGS = 208, SHR_OTHER_REGS = 88;
 static_assert(8 * SHR_SOFTMAX_REGS + 4 * SHR_OTHER_REGS <= 12 * ATT_LAUNCH_REGS, "the increase must fit in what the others give back");
-constexpr int SHR_PRODUCER_WARP = 3, SHR_MMA_WARP = 2;
+constexpr int SHR_PRODUCER_WARP = 3, SHR_MMA_WARP0 = 1, SHR_ALLOC_WARP = 0;
 constexpr float SHR_P_SCALE_LOG2 = 7.0f;
 
 struct SharedParams {
@@ -65,7 +65,7 @@ struct SharedSmem {
     static constexpr int K_BYTES = SHR_PAGES * BOX_BYTES;             // K (or V) of a stage
     static constexpr int Q_HALF = 128 * 128, Q_BYTES = HALVES * Q_HALF;   // a tile: [half][128 rows][128 bytes]
     static constexpr int K_SLOTS = HD == 128 ? 2 : 5, V_SLOTS = HD == 128 ? 3 : 6;
-    static constexpr int TOTAL = 1024 + 2 * Q_BYTES + (K_SLOTS + V_SLOTS) * K_BYTES + 512;
+    static constexpr int TOTAL = 1024 + 2 * Q_BYTES + (K_SLOTS + V_SLOTS) * K_BYTES + SHR_BAR_BYTES;
     static_assert(TOTAL <= 232448, "shared memory of one CTA");
     static constexpr int TMEM_COLS = 512;   // O of the two groups at 0 and 128; S (and P) at 256 and 384
 };
@@ -90,19 +90,22 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     uint8_t* qbuf = smem;                               // two slots
     uint8_t* kring = qbuf + 2 * SM::Q_BYTES;
     uint8_t* vring = kring + KS * SM::K_BYTES;
-    // (A wait on a phase's parity must not be two phases off: whoever waits on a barrier has to see every one of its phases.)
-    uint64_t* k_full = reinterpret_cast<uint64_t*>(vring + VS * SM::K_BYTES);
-    uint64_t* k_empty = k_full + KS;     // every score of the stage is complete
-    uint64_t* v_full = k_empty + KS;
-    uint64_t* v_empty = v_full + VS;     // every P V of the stage is complete
+    // A wait on a phase's parity must not be two phases off: whoever waits on a barrier has to see every one of its phases.  So
+    // a slot has three "full" barriers, for stages of group 0, of group 1 and of both, and the Q slots are watched by both issuers.
+    // "Empty" barriers count two commits: both issuers' where both use the slot, twice the one's where it is the only one.
+    uint64_t* k_full = reinterpret_cast<uint64_t*>(vring + VS * SM::K_BYTES);   // [who][slot]
+    uint64_t* k_empty = k_full + 3 * KS; // every score of the stage is complete
+    uint64_t* v_full = k_empty + KS;     // [who][slot]
+    uint64_t* v_empty = v_full + 3 * VS; // every P V of the stage is complete
     uint64_t* q_full = v_empty + VS;     // [slot]
     uint64_t* q_empty = q_full + 2;      // [slot] the last Q K^T that reads it is complete
-    uint64_t* s_full = q_empty + 2;      // [group] scores of a stage (and every P V before) are complete
-    uint64_t* p_full = s_full + 2;       // [group] P of a stage is in tensor memory (and O rescaled if need be)
-    uint64_t* o_full = p_full + 2;       // [group] the item's last P V is complete
+    uint64_t* s_full = q_empty + 2;      // [group][buffer] scores of a half stage (and what was issued before them) are complete
+    uint64_t* p_full = s_full + 4;       // [group][buffer] P of a half stage is in tensor memory (and O rescaled if need be)
+    uint64_t* pv_done = p_full + 4;      // [group] a P V is complete
+    uint64_t* o_full = pv_done + 2;      // [group] the item's last P V is complete
     uint64_t* o_empty = o_full + 2;      // [group] its warps have read O
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_empty + 2);
-    static_assert((2 * KS + 2 * VS + 12) * 8 + 4 <= 512, "barrier area");
+    static_assert((4 * KS + 4 * VS + 18) * 8 + 4 <= SHR_BAR_BYTES, "barrier area");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int it_begin = p.cta_begin[blockIdx.x], it_end = p.cta_begin[blockIdx.x + 1];
@@ -112,20 +115,25 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     if (threadIdx.x == 0) {
         tma_prefetch_desc(&tmQ);
         tma_prefetch_desc(&tmKV);
-        for (int s = 0; s < KS; ++s) { mbar_init(&k_full[s], 1); mbar_init(&k_empty[s], 1); }
-        for (int s = 0; s < VS; ++s) { mbar_init(&v_full[s], 1); mbar_init(&v_empty[s], 1); }
+        for (int s = 0; s < 3 * KS; ++s) mbar_init(&k_full[s], 1);
+        for (int s = 0; s < 3 * VS; ++s) mbar_init(&v_full[s], 1);
+        for (int s = 0; s < KS; ++s) mbar_init(&k_empty[s], 2);
+        for (int s = 0; s < VS; ++s) mbar_init(&v_empty[s], 2);
         for (int s = 0; s < 2; ++s) {
             mbar_init(&q_full[s], 1);
-            mbar_init(&q_empty[s], 1);
-            mbar_init(&s_full[s], 1);
-            mbar_init(&p_full[s], 4);
+            mbar_init(&q_empty[s], 2);
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(&s_full[2 * s + b], 1);
+                mbar_init(&p_full[2 * s + b], 4);
+            }
+            mbar_init(&pv_done[s], 1);
             mbar_init(&o_full[s], 1);
             mbar_init(&o_empty[s], 4);
         }
         mbar_fence_init();
         if (!list_ok) atomicExch(p.status, 2);
     }
-    if (warp == SHR_MMA_WARP) {
+    if (warp == SHR_ALLOC_WARP) {
         tmem_alloc(tmem_slot, SM::TMEM_COLS);
         tmem_relinquish();
     }
@@ -180,7 +188,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll
                     for (int v = 0; v < 2; ++v) {
                         const uint32_t n = v ? VS : KS, s = st % n;
-                        uint64_t* full = v ? v_full : k_full;
+                        uint64_t* full = (v ? v_full : k_full) + (item.tiles == 2 ? 2 : k & 1) * n;
                         if (lane == 0) {
                             if (st >= n) ok = mbar_wait(&(v ? v_empty : k_empty)[s], ((st / n) - 1) & 1u, p.status);
                             if (ok) mbar_expect_tx(&full[s], (uint32_t)npg * SM::BOX_BYTES);
@@ -193,84 +201,116 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                     if (!ok) break;
                 }
             }
-        } else if (warp == SHR_MMA_WARP && elect_one()) {
-            // -------------------------------------------------------- MMA issuer
-            // The groups take turns: P V of a group's stage, Q K^T of its next, then the other group's.  In this order, which
-            // the tensor cores keep, one group's scores are ready half a stage's time before the other's, so that one computes
-            // exponentials while the products of the other run (issued by whichever is ready, the two fall into step: both
-            // compute, then both wait; 5 300 cycles a stage instead of SHR_STAGE2).  A group's P V waits for its turn in the next item.
-            const uint32_t idesc_pv = umma_idesc_f16_bmn(128, HD), idesc_qk = umma_idesc_f16(128, SHARED_STAGE);
-            struct Pending { uint32_t pages, vs, v_parity; bool any, first, last, wait_v, free_v; };   // a group's P V to come
-            Pending pend[2];
-            pend[0].any = pend[1].any = false;
-            uint32_t use[2] = {0, 0}, o_use[2] = {0, 0};   // P V's of each group so far, and items among them
-            uint32_t st = 0, qs = 0;                       // stage and Q slot of the item's first
+        } else if ((warp == SHR_MMA_WARP0 || warp == SHR_MMA_WARP0 + 1) && elect_one()) {
+            // -------------------------------------------------------- MMA issuers, one a group
+            // A group works through half stages of 64 keys with two score buffers: the scores of half u + 1 are there while it
+            // computes the weights of half u.  Its issuer's turn: P V of half u - 2, then Q K^T of half u into the buffer that this
+            // P V has read (operations of one thread complete in order).  One thread for both groups was the bound: a turn takes it
+            // about 1 200 cycles, the group's weights of a half stage 1 100.
+            const int w = warp - SHR_MMA_WARP0;
+            const uint32_t idesc_pv = umma_idesc_f16_bmn(128, HD), idesc_qk = umma_idesc_f16(128, SHR_HALF);
+            const uint32_t o_tmem = tmem_base + w * 128, s_tmem0 = tmem_base + 256 + w * 128;
+            const uint64_t k_desc0 = umma_desc_k128s(smem_u32(kring), SM::GROUP_BYTES), v_desc0 = umma_desc_mn128(smem_u32(vring), 1024, SM::GROUP_BYTES);
+            constexpr uint32_t SLOT16 = SM::K_BYTES >> 4, HALF16 = SLOT16 / 2;
+            // P V's to come, at most two, the older first: pages | V slot << 4 | half << 8 | first << 9 | last << 10 | wait for V << 11 |
+            // its phase's parity << 12 | end of the stage << 13 | stage of both << 14; and the older one's stage
+            uint32_t todo0 = 0, todo1 = 0, stage0 = 0, stage1 = 0, n_todo = 0;
+            uint32_t use = 0, o_use = 0;     // P V's so far, and items among them
+            uint32_t st = 0, qs = 0;         // stage and Q slot of the item's first
+            uint32_t k_own = 0, k_both = 0, v_own = 0, v_both = 0;   // bit s: parity of the next phase of slot s
             bool ok = true;
-            auto pv = [&](int w) {
-                const Pending& n = pend[w];
-                pend[w].any = false;
-                ok = mbar_wait(&p_full[w], use[w] & 1u, p.status);
-                if (ok && n.wait_v) ok = mbar_wait(&v_full[n.vs], n.v_parity, p.status);
-                if (ok && n.first && o_use[w] > 0) ok = mbar_wait(&o_empty[w], (o_use[w] - 1) & 1u, p.status);
+            auto pv = [&]() {
+                const uint32_t f = todo0, pages = f & 15u, vs = (f >> 4) & 15u, buf = use & 1u;
+                todo0 = todo1;
+                stage0 = stage1;
+                --n_todo;
+                const bool first = (f >> 9) & 1u;
+                if ((f >> 11) & 1u) ok = mbar_wait(&v_full[((f >> 14) & 1u ? 2 : w) * VS + vs], (f >> 12) & 1u, p.status);
+                if (ok && first && o_use > 0) ok = mbar_wait(&o_empty[w], (o_use - 1) & 1u, p.status);
+                if (ok) ok = mbar_wait(&p_full[2 * w + buf], (use >> 1) & 1u, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                const uint32_t s_tmem = tmem_base + 256 + w * 128, o_tmem = tmem_base + w * 128;
-                const uint64_t b = umma_desc_mn128(smem_u32(vring + n.vs * SM::K_BYTES), 1024, SM::GROUP_BYTES);
-                if (n.pages == SHR_PAGES) {
+                const uint32_t p_tmem = s_tmem0 + buf * 64;
+                const uint64_t b = v_desc0 + vs * SLOT16 + ((f >> 8) & 1u) * HALF16;
 #pragma unroll
-                    for (uint32_t i = 0; i < SHR_PAGES; ++i)   // step i: the 16 keys of a page; an item's first P V starts its O afresh
-                        umma_f16_ta(o_tmem, s_tmem + 8 * i, b + i * (SM::BOX_BYTES >> 4), idesc_pv, !n.first || i != 0);
-                } else {
-                    for (uint32_t i = 0; i < n.pages; ++i) umma_f16_ta(o_tmem, s_tmem + 8 * i, b + i * (SM::BOX_BYTES >> 4), idesc_pv, !n.first || i != 0);
+                for (uint32_t i = 0; i < SHR_PAGES / 2; ++i)   // step i: the 16 keys of a page; an item's first P V starts its O afresh
+                    if (i < pages) umma_f16_ta(o_tmem, p_tmem + 8 * i, b + i * (SM::BOX_BYTES >> 4), idesc_pv, !first || i != 0);
+                umma_commit(&pv_done[w]);
+                if ((f >> 13) & 1u) {
+                    umma_commit(&v_empty[vs]);
+                    if (!((f >> 14) & 1u)) umma_commit(&v_empty[vs]);
                 }
-                if (n.free_v) umma_commit(&v_empty[n.vs]);
-                if (n.last) {
+                if ((f >> 10) & 1u) {
                     umma_commit(&o_full[w]);
-                    ++o_use[w];
+                    ++o_use;
                 }
-                ++use[w];
+                ++use;
             };
             for (int it = it_begin; list_ok && it < it_end && ok; ++it) {
                 const SharedItem item = p.items[it];
                 if (!shared_item_ok(item, p)) break;
                 const bool two = item.tiles == 2;
-                const int keys = item.kv_end - item.kv_begin;
-                const uint32_t n_st = (uint32_t)(keys + SHARED_STAGE - 1) / SHARED_STAGE, step = two ? 1 : 2;
+                const int n_pages = (item.kv_end - item.kv_begin + 15) >> 4;
+                const uint32_t n_st = (uint32_t)(n_pages + SHR_PAGES - 1) / SHR_PAGES, step = two ? 1 : 2;
+                const uint64_t a = umma_desc_k128(smem_u32(qbuf + ((qs + (two ? w : 0)) & 1u) * SM::Q_BYTES));
+                // The producer requests K of stage s behind V of stage s - 1: no P V that holds a slot it needs may be pending when K (or
+                // Q) is waited for (one would be, of the second group, through any number of items of one stage).
+                while (ok && n_todo > 0 && (int)stage0 <= (int)st - VS) pv();
                 for (uint32_t q = qs; q < qs + item.tiles && ok; ++q) ok = mbar_wait(&q_full[q & 1u], (q >> 1) & 1u, p.status);
-                for (uint32_t k0 = 0; k0 < n_st && ok; k0 += step) {
+                if (!ok) break;
+                uint32_t kb = two ? k_both : k_own, vb = two ? v_both : v_own;
+                if (!two && (uint32_t)w >= n_st) mbar_arrive(&q_empty[qs & 1u]);   // nothing here for the second group
+                uint32_t k = two ? 0 : w, ks = (st + k) % KS, vs = (st + k) % VS;
+                for (; k < n_st && ok; k += step) {
+                    const uint32_t s = st + k, pages = (uint32_t)min(SHR_PAGES, n_pages - (int)k * SHR_PAGES);
+                    while (ok && n_todo > 0 && (int)stage0 <= (int)s - VS) pv();
+                    if (ok) ok = mbar_wait(&k_full[(two ? 2 : w) * KS + ks], (kb >> ks) & 1u, p.status);
+                    if (!ok) break;
+                    const uint32_t v_parity = (vb >> vs) & 1u;
+                    kb ^= 1u << ks;
+                    vb ^= 1u << vs;
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const uint32_t k = two ? k0 : k0 + w;
-                        if (k >= n_st || !ok) continue;
-                        if (pend[w].any) pv(w);
-                        const uint32_t s = st + k, ks = s % KS;
-                        const uint32_t pages = (uint32_t)min(SHR_PAGES, (keys - (int)k * SHARED_STAGE + 15) >> 4);
-                        if (ok && (!two || w == 0)) ok = mbar_wait(&k_full[ks], (s / KS) & 1u, p.status);   // (seen by the other's turn)
+                    for (uint32_t h = 0; h < 2; ++h) {
+                        if (!ok || h * (SHR_PAGES / 2) >= pages) continue;
+                        if (n_todo == 2) pv();
                         if (!ok) continue;
                         tc_fence_after();
-                        const uint32_t s_tmem = tmem_base + 256 + w * 128;
-                        const uint64_t a = umma_desc_k128(smem_u32(qbuf + ((qs + (two ? w : 0)) & 1u) * SM::Q_BYTES));
-                        const uint64_t b = umma_desc_k128s(smem_u32(kring + ks * SM::K_BYTES), SM::GROUP_BYTES);
-                        const uint32_t idesc = pages == SHR_PAGES ? idesc_qk : umma_idesc_f16(128, 16 * pages);
+                        const uint32_t here = min((uint32_t)SHR_PAGES / 2, pages - h * (SHR_PAGES / 2)), buf = (use + n_todo) & 1u;
+                        const uint32_t s_tmem = s_tmem0 + buf * 64;
+                        const uint64_t b = k_desc0 + ks * SLOT16 + h * HALF16;
+                        const uint32_t idesc = here == SHR_PAGES / 2 ? idesc_qk : umma_idesc_f16(128, 16 * here);
 #pragma unroll
                         for (uint32_t i = 0; i < HD / 16; ++i)   // step i: 16 dims, of the second half from step 4 on
                             umma_bf16(s_tmem, a + (i >> 2) * (SM::Q_HALF >> 4) + 2 * (i & 3), b + (i >> 2) * (1024 >> 4) + 2 * (i & 3), idesc, i != 0);
-                        umma_commit(&s_full[w]);
-                        const bool all = !two || w == 1;         // nobody else has the stage to come
-                        if (all) umma_commit(&k_empty[ks]);
-                        if (all && k == n_st - 1)
+                        umma_commit(&s_full[2 * w + buf]);
+                        const bool end = (h + 1) * (SHR_PAGES / 2) >= pages, first = k < step && h == 0, last = k + step >= n_st && end;
+                        if (end) {
+                            umma_commit(&k_empty[ks]);
+                            if (!two) umma_commit(&k_empty[ks]);
+                        }
+                        if (last)
                             for (uint32_t q = qs; q < qs + item.tiles; ++q) umma_commit(&q_empty[q & 1u]);
-                        pend[w] = Pending{pages, s % VS, (s / VS) & 1u, true, k < step, k + step >= n_st, !two || w == 0, all};
+                        const uint32_t f = here | vs << 4 | h << 8 | (uint32_t)first << 9 | (uint32_t)last << 10 | (uint32_t)(h == 0) << 11 | v_parity << 12 |
+                                           (uint32_t)end << 13 | (uint32_t)two << 14;
+                        if (n_todo == 0) {
+                            todo0 = f;
+                            stage0 = s;
+                        }
+                        todo1 = f;
+                        stage1 = s;
+                        ++n_todo;
                     }
+                    ks += step;
+                    if (ks >= (uint32_t)KS) ks -= KS;
+                    vs += step;
+                    if (vs >= (uint32_t)VS) vs -= VS;
                 }
-                // an odd number of turns: the second group's P V is older than the first's, and its V slot is needed before its turn
-                // would come again (after any number of items of one stage)
-                if (ok && !two && (n_st & 1) && pend[1].any) pv(1);
+                (two ? k_both : k_own) = kb;
+                (two ? v_both : v_own) = vb;
                 st += n_st;
                 qs += item.tiles;
             }
-            for (int w = 0; w < 2; ++w)
-                if (ok && pend[w].any) pv(w);
+            while (ok && n_todo > 0) pv();
         }
         __syncwarp();
     } else {
@@ -281,6 +321,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const uint32_t t_lane = tmem_base + ((uint32_t)(wq * 32) << 16);
         const uint32_t o_col = (uint32_t)wg * 128, s_col = 256 + (uint32_t)wg * 128;
         uint32_t st = 0, use = 0, o_use = 0;
+        uint32_t v_own = 0, v_both = 0;   // as the issuer's
         bool ok = true;   // uniform over the warp: the tensor-memory loads and stores are warp-wide
         auto wait_all = [&](uint64_t* bar, uint32_t parity) {
             const bool r = mbar_wait(bar, parity, p.status);
@@ -300,91 +341,104 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             const int n_st = (item.kv_end - item.kv_begin + SHARED_STAGE - 1) / SHARED_STAGE;
             const int lim = item.q_pos0 + first_tok + row / G;        // last visible key position of this row
             float m_used = -INFINITY, l = 0.f;
-            int mine = 0;                                             // stages of this group
+            int mine = 0;                                             // half stages of this group
+            const Two scale2 = two_of(p.scale_log2, p.scale_log2);
             for (int k = 0; k < n_st; ++k) {
                 if (!two && (k & 1) != wg) continue;
-                const int kv0 = item.kv_begin + k * SHARED_STAGE;
-                if (ok) ok = wait_all(&s_full[wg], use & 1u);
-                ++use;
-                if (wlive && ok) {
-                    uint32_t s[4][32];
-                    tc_fence_after();
+                const uint32_t vs = (uint32_t)(st + k) % VS, v_parity = ((two ? v_both : v_own) >> vs) & 1u;
+                (two ? v_both : v_own) ^= 1u << vs;
+                for (int kv0 = item.kv_begin + k * SHARED_STAGE, h = 0; h < 2 && kv0 < item.kv_end; ++h, kv0 += SHR_HALF, ++use, ++mine) {
+                    const uint32_t buf = use & 1u, s_tmem = t_lane + s_col + buf * 64;
+                    if (ok) ok = wait_all(&s_full[2 * wg + buf], (use >> 1) & 1u);
+                    if (wlive && ok) {
+                        uint32_t s[2][32];
+                        tc_fence_after();
+                        tmem_ld32(s_tmem, s[0]);
+                        tmem_ld32(s_tmem + 32, s[1]);
+                        tmem_ld_wait();
+                        // keys this row sees in the half stage: positions < min(kv_end, lim + 1)
+                        const int nvalid = min(item.kv_end, lim + 1) - kv0;
+                        if (nvalid < SHR_HALF) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(t_lane + s_col + 32 * c, s[c]);
-                    tmem_ld_wait();
-                    // keys this row sees in the stage: positions < min(kv_end, lim + 1)
-                    const int nvalid = min(item.kv_end, lim + 1) - kv0;
-                    if (nvalid < SHARED_STAGE) {
+                            for (int c = 0; c < 2; ++c)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)
+                                for (int i = 0; i < 32; ++i)
+                                    if (32 * c + i >= nvalid) s[c][i] = 0xFF800000u;   // -inf
+                        }
+                        float mc[4];
 #pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (32 * c + i >= nvalid) s[c][i] = 0xFF800000u;   // -inf
-                    }
-                    float mc[4];
+                        for (int c = 0; c < 4; ++c) {
+                            const uint32_t* x = &s[c >> 1][(c & 1) * 16];
+                            mc[c] = __uint_as_float(x[0]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        mc[c] = __uint_as_float(s[c][0]);
-#pragma unroll
-                        for (int i = 1; i < 32; ++i) mc[c] = fmaxf(mc[c], __uint_as_float(s[c][i]));
-                    }
-                    const float ms = fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3])) * p.scale_log2;
-                    if (mine == 0) {
-                        m_used = live ? ms : 0.f;
-                    } else {
-                        const bool grow = live && ms > m_used + ATT2_RESCALE_GAP;
-                        if (__any_sync(0xFFFFFFFFu, grow)) {
-                            const float corr = grow ? ex2_approx(m_used - ms) : 1.f;   // (P V of the stage before is complete: s_full)
-                            if (grow) {
-                                m_used = ms;
-                                l *= corr;
-                            }
+                            for (int i = 1; i < 15; i += 2) mc[c] = max3(mc[c], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+                            mc[c] = fmaxf(mc[c], __uint_as_float(x[15]));
+                        }
+                        const float ms = fmaxf(max3(mc[0], mc[1], mc[2]), mc[3]) * p.scale_log2;
+                        if (mine == 0) {
+                            m_used = live ? ms : 0.f;
+                        } else {
+                            const bool grow = live && ms > m_used + ATT2_RESCALE_GAP;
+                            if (__any_sync(0xFFFFFFFFu, grow)) {
+                                // O is rescaled in tensor memory: the P V before must have completed.  (Those before it have: the scores
+                                // waited for above were issued behind them.  So this phase's parity is unmistakable.)
+                                ok = wait_all(&pv_done[wg], (use - 1) & 1u);
+                                const float corr = grow ? ex2_approx(m_used - ms) : 1.f;
+                                if (grow) {
+                                    m_used = ms;
+                                    l *= corr;
+                                }
+                                tc_fence_after();
 #pragma unroll 1
-                            for (int ch = 0; ch < HD / 16; ++ch) {
-                                uint32_t o[16];
-                                tmem_ld16(t_lane + o_col + ch * 16, o);
-                                tmem_ld_wait();
+                                for (int ch = 0; ok && ch < HD / 16; ++ch) {
+                                    uint32_t o[16];
+                                    tmem_ld16(t_lane + o_col + ch * 16, o);
+                                    tmem_ld_wait();
 #pragma unroll
-                                for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * corr);
-                                tmem_st16(t_lane + o_col + ch * 16, o);
+                                    for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * corr);
+                                    tmem_st16(t_lane + o_col + ch * 16, o);
+                                }
                             }
                         }
-                    }
-                    const float base = (m_used == -INFINITY ? 0.f : m_used) - SHR_P_SCALE_LOG2;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                        const float base = (m_used == -INFINITY ? 0.f : m_used) - SHR_P_SCALE_LOG2;
+                        const Two base2 = two_of(-base, -base);
+                        Two sum[2] = {two_of(0.f, 0.f), two_of(0.f, 0.f)};
+                        uint32_t pw[2][16];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t pw[16];
+                        for (int c = 0; c < 2; ++c) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float a = ex2_approx(fmaf(__uint_as_float(s[c][2 * i]), p.scale_log2, -base));
-                            const float b = ex2_approx(fmaf(__uint_as_float(s[c][2 * i + 1]), p.scale_log2, -base));
-                            sum[i & 3] += a + b;
-                            pw[i] = pack_op(a, b);   // (rows beyond the tile's hold garbage: they only meet themselves in the products)
+                            for (int i = 0; i < 16; ++i) {
+                                float a, b;
+                                untwo(fma2(two_of(__uint_as_float(s[c][2 * i]), __uint_as_float(s[c][2 * i + 1])), scale2, base2), a, b);
+                                a = ex2_approx(a);
+                                b = ex2_approx(b);
+                                sum[i & 1] = add2(sum[i & 1], two_of(a, b));
+                                pw[c][i] = pack_op(a, b);   // (rows beyond the tile's hold garbage: they only meet themselves in the products)
+                            }
+                            if (ok) tmem_st16(s_tmem + 16 * c, pw[c]);
                         }
-                        tmem_st16(t_lane + s_col + 16 * c, pw);
+                        float u0, u1;
+                        untwo(add2(sum[0], sum[1]), u0, u1);
+                        l += u0 + u1;
+                        tmem_st_wait();
+                        tc_fence_before();
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                    tmem_st_wait();
-                    tc_fence_before();
-                }
-                // Rows of the last page behind the item's keys: a weight of zero takes whatever is stale there out, unless that is no
-                // number.  Every group that uses the stage clears them before its P V can start.
-                if ((item.kv_end & 15) && k == n_st - 1 && ok) {
-                    const uint32_t vs = (st + k) % VS;
-                    // (its phase before is over: the scores of this stage were issued behind the P V that used the slot)
-                    ok = wait_all(&v_full[vs], ((st + k) / VS) & 1u);
-                    uint8_t* box = vring + vs * SM::K_BYTES + ((item.kv_end - 1 - kv0) >> 4) * SM::BOX_BYTES;
-                    const int r0 = item.kv_end & 15;
-                    for (int c = row; ok && c < (16 - r0) * HALVES * 8; c += 128) {
-                        const int r = r0 + c / (HALVES * 8), h = (c >> 3) % HALVES;
-                        *reinterpret_cast<uint4*>(box + (r >> 3) * SM::GROUP_BYTES + h * 1024 + (r & 7) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    // Rows of the last page behind the item's keys: a weight of zero takes whatever is stale there out, unless that is no
+                    // number.  Every group that uses the stage clears them before its P V can start.
+                    if ((item.kv_end & 15) && kv0 + SHR_HALF >= item.kv_end && ok) {
+                        // (the phase before is over: the issuer has seen it before this stage's scores)
+                        ok = wait_all(&v_full[(two ? 2 : wg) * VS + vs], v_parity);
+                        uint8_t* box = vring + vs * SM::K_BYTES + ((item.kv_end - 1 - item.kv_begin) / 16 - k * SHR_PAGES) * SM::BOX_BYTES;
+                        const int r0 = item.kv_end & 15;
+                        for (int c = row; ok && c < (16 - r0) * HALVES * 8; c += 128) {
+                            const int r = r0 + c / (HALVES * 8), half = (c >> 3) % HALVES;
+                            *reinterpret_cast<uint4*>(box + (r >> 3) * SM::GROUP_BYTES + half * 1024 + (r & 7) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_proxy_async_smem();
                     }
-                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0 && ok) mbar_arrive(&p_full[2 * wg + buf]);
                 }
-                __syncwarp();
-                if (lane == 0 && ok) mbar_arrive(&p_full[wg]);
-                ++mine;
             }
             st += n_st;
             if (mine == 0) continue;   // one tile, one stage: the second group has no part in it
@@ -415,7 +469,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     // ---------------------------------------------------------------- teardown
     tc_fence_before();
     __syncthreads();
-    if (warp == SHR_MMA_WARP) {
+    if (warp == SHR_ALLOC_WARP) {
         tc_fence_after();
         tmem_dealloc(tmem_base, SM::TMEM_COLS);
     }

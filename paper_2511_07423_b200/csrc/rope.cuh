@@ -158,25 +158,6 @@ struct RopeLane {
     }
 };
 
-// Two fp32 values that the arithmetic units take at a time.
-struct Two { unsigned long long v; };
-__device__ __forceinline__ Two two(float x, float y) {
-    Two r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ void untwo(Two t, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(t.v)); }
-__device__ __forceinline__ Two mul2(Two a, Two b) {
-    Two r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-    Two r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
-
 // A warp takes one token and some heads of one segment (blockIdx.y: which), U accesses' worth of heads at a time.
 // Gains and angles are the same for all heads of a token, so they are multiplied into four factors a pair once:
 // y_a = r (x_a gain_a cos - x_b gain_b sin), y_b = r (x_b gain_b cos + x_a gain_a sin), r = 1 / sqrt(mean x^2 + eps).
@@ -234,10 +215,10 @@ rope_kernel(const __grid_constant__ RopeParams p) {
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        aa[j] = two(ga[2 * j] * c[2 * j], ga[2 * j + 1] * c[2 * j + 1]);
-        ab[j] = two(-gb[2 * j] * s[2 * j], -gb[2 * j + 1] * s[2 * j + 1]);
-        bb[j] = two(gb[2 * j] * c[2 * j], gb[2 * j + 1] * c[2 * j + 1]);
-        ba[j] = two(ga[2 * j] * s[2 * j], ga[2 * j + 1] * s[2 * j + 1]);
+        aa[j] = two_of(ga[2 * j] * c[2 * j], ga[2 * j + 1] * c[2 * j + 1]);
+        ab[j] = two_of(-gb[2 * j] * s[2 * j], -gb[2 * j + 1] * s[2 * j + 1]);
+        bb[j] = two_of(gb[2 * j] * c[2 * j], gb[2 * j + 1] * c[2 * j + 1]);
+        ba[j] = two_of(ga[2 * j] * s[2 * j], ga[2 * j + 1] * s[2 * j + 1]);
     }
     TOUT* y = reinterpret_cast<TOUT*>(sg.y) + t * sg.y_stride;
     op16* row = p.pool + ((int64_t)(slot >> 4) * p.n_kv_heads * 2 + sg.plane) * 16 * hd + (slot & 15) * hd;
@@ -247,8 +228,8 @@ rope_kernel(const __grid_constant__ RopeParams p) {
             Two xa[2], xb[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                xa[j] = two(a[i][2 * j], a[i][2 * j + 1]);
-                xb[j] = two(b[i][2 * j], b[i][2 * j + 1]);
+                xa[j] = two_of(a[i][2 * j], a[i][2 * j + 1]);
+                xb[j] = two_of(b[i][2 * j], b[i][2 * j + 1]);
             }
             if (norm) {
                 const Two sq = fma2(xb[1], xb[1], fma2(xa[1], xa[1], fma2(xb[0], xb[0], mul2(xa[0], xa[0]))));
@@ -261,8 +242,8 @@ rope_kernel(const __grid_constant__ RopeParams p) {
                 const float r = rsqrtf(fmaf(ss, p.inv_hd, p.eps));
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    xa[j] = mul2(xa[j], two(r, r));
-                    xb[j] = mul2(xb[j], two(r, r));
+                    xa[j] = mul2(xa[j], two_of(r, r));
+                    xb[j] = mul2(xb[j], two_of(r, r));
                 }
             }
             Two ya[2], yb[2];
