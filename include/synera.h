@@ -250,8 +250,9 @@ int syn_plan_work_host(const syn_model_desc *desc, uint32_t n_pages, uint32_t pa
 /* The work list of syn_plan_create_shared on n_sm SMs (at most 32767), whether or not the planner would take it (*taken); arguments and
  * validation as in syn_plan_host.  items [items_cap][SYN_SHARED_ITEM_FIELDS], in CTA order: (first query token, query tokens,
  * kv head, request whose page table is read, first key, one past the last key, position of the first query token or -1 where
- * every token sees every key, first row of its partial results, tiles of rows 1 or 2).  parts [parts_cap][3]: (token, kv head, row), sorted by the first
- * two: the rows of partial results that are merged for the kv head's first query head; an item of one tile and more than one stage of 128 keys
+ * every token sees every key, first row of its partial results, mode: 0 or 1 one tile of 128 rows, the whole item one group of warps,
+ * 2 two tiles, a group each, 3 one tile, the groups take alternate stages of 128 keys).  parts [parts_cap][3]: (token, kv head, row), sorted by the first
+ * two: the rows of partial results that are merged for the kv head's first query head; an item of mode 3
  * leaves two, of its even and its odd stages.  SYN_E_CAPACITY if a capacity is too small, *n_items and *n_parts then hold the counts needed; NULL to
  * skip an array.  stats may be NULL. */
 #define SYN_SHARED_ITEM_FIELDS 9

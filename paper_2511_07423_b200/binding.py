@@ -571,7 +571,7 @@ def plan_work_host(shape, n_pages: int, chunk_tokens, chunk_offsets, page_tables
     return {"items": items, "cta_begin": cta[:n_cta.value + 1], "n_cta": n_cta.value, "attention": kind.value, "stats": st}
 
 
-SHARED_ITEM_FIELDS = ("q_tok", "n_tok", "kvh", "req", "kv_begin", "kv_end", "q_pos0", "base", "tiles")
+SHARED_ITEM_FIELDS = ("q_tok", "n_tok", "kvh", "req", "kv_begin", "kv_end", "q_pos0", "base", "mode")
 
 
 def plan_shared_host(shape, n_pages: int, chunk_tokens, chunk_offsets, page_tables, ctx_lens, n_uncached=None,

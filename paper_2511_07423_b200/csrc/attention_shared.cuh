@@ -51,8 +51,9 @@ struct SharedParams {
 // The work list is host-made; the kernel still refuses an item that would index out of bounds.
 __device__ __forceinline__ bool shared_item_ok(const SharedItem& it, const SharedParams& p) {
     const int stages = (it.kv_end - it.kv_begin + SHARED_STAGE - 1) / SHARED_STAGE;
-    const int64_t rows = (int64_t)it.n_tok * p.group * (it.tiles == 1 && stages > 1 ? 2 : 1);
-    return it.q_tok >= 0 && it.n_tok >= 1 && it.q_tok + it.n_tok <= p.n_tokens && (it.tiles == 1 || it.tiles == 2) && it.n_tok <= it.tiles * p.tile_tokens &&
+    const int64_t rows = (int64_t)it.n_tok * p.group * (it.mode == SHARED_STAGES ? 2 : 1);
+    return it.q_tok >= 0 && it.n_tok >= 1 && it.q_tok + it.n_tok <= p.n_tokens && it.mode >= 0 && it.mode <= 3 &&
+           it.n_tok <= (it.mode == SHARED_TILES ? 2 : 1) * p.tile_tokens && (it.mode != SHARED_STAGES || stages > 1) &&
            it.kvh >= 0 && it.kvh < p.n_kv_heads && it.req >= 0 && it.req < p.n_req && it.kv_begin >= 0 && (it.kv_begin & 15) == 0 &&
            it.kv_begin < it.kv_end && ((it.kv_end - 1) >> 4) < p.max_pages && it.base >= 0 && it.base + rows <= p.n_rows;
 }
@@ -64,6 +65,7 @@ struct SharedSmem {
     static constexpr int BOX_BYTES = 2 * GROUP_BYTES;                 // the K rows (or the V rows) of a page
     static constexpr int K_BYTES = SHR_PAGES * BOX_BYTES;             // K (or V) of a stage
     static constexpr int Q_HALF = 128 * 128, Q_BYTES = HALVES * Q_HALF;   // a tile: [half][128 rows][128 bytes]
+    static constexpr int OUT_COLS = HD / 4;                           // columns that the epilogue turns around at a time: 128 rows in half a Q tile
     static constexpr int K_SLOTS = HD == 128 ? 2 : 5, V_SLOTS = HD == 128 ? 3 : 6;
     static constexpr int TOTAL = 1024 + 2 * Q_BYTES + (K_SLOTS + V_SLOTS) * K_BYTES + SHR_BAR_BYTES;
     static_assert(TOTAL <= 232448, "shared memory of one CTA");
@@ -79,6 +81,12 @@ __device__ __forceinline__ void umma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, ui
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+
+// The exponentials of the two groups' warps that share a scheduler, one warp after the other (a named barrier of each, which the
+// other arrives on when it is done): in step they would compete for the special-function unit and then leave it idle
+// together.  Both groups have as many turns (items of two tiles); the second group's first arrival lets the first begin.
+__device__ __forceinline__ void shr_turn(int wg, int wq) { asm volatile("bar.sync %0, 64;" ::"r"(1 + wg * 4 + wq) : "memory"); }
+__device__ __forceinline__ void shr_turn_over(int wg, int wq) { asm volatile("bar.arrive %0, 64;" ::"r"(1 + (wg ^ 1) * 4 + wq) : "memory"); }
 
 template <int HD>
 __global__ void __launch_bounds__(SHR_THREADS, 1)
@@ -98,14 +106,15 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     uint64_t* v_full = k_empty + KS;     // [who][slot]
     uint64_t* v_empty = v_full + 3 * VS; // every P V of the stage is complete
     uint64_t* q_full = v_empty + VS;     // [slot]
-    uint64_t* q_empty = q_full + 2;      // [slot] the last Q K^T that reads it is complete
+    uint64_t* q_done = q_full + 2;       // [slot] the last Q K^T that reads it is complete
+    uint64_t* q_empty = q_done + 2;      // [slot] nor do the softmax warps use it any more
     uint64_t* s_full = q_empty + 2;      // [group][buffer] scores of a half stage (and what was issued before them) are complete
     uint64_t* p_full = s_full + 4;       // [group][buffer] P of a half stage is in tensor memory (and O rescaled if need be)
     uint64_t* pv_done = p_full + 4;      // [group] a P V is complete
     uint64_t* o_full = pv_done + 2;      // [group] the item's last P V is complete
     uint64_t* o_empty = o_full + 2;      // [group] its warps have read O
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_empty + 2);
-    static_assert((4 * KS + 4 * VS + 18) * 8 + 4 <= SHR_BAR_BYTES, "barrier area");
+    static_assert((4 * KS + 4 * VS + 20) * 8 + 4 <= SHR_BAR_BYTES, "barrier area");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int it_begin = p.cta_begin[blockIdx.x], it_end = p.cta_begin[blockIdx.x + 1];
@@ -121,7 +130,8 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         for (int s = 0; s < VS; ++s) mbar_init(&v_empty[s], 2);
         for (int s = 0; s < 2; ++s) {
             mbar_init(&q_full[s], 1);
-            mbar_init(&q_empty[s], 2);
+            mbar_init(&q_done[s], 2);
+            mbar_init(&q_empty[s], 8);
             for (int b = 0; b < 2; ++b) {
                 mbar_init(&s_full[2 * s + b], 1);
                 mbar_init(&p_full[2 * s + b], 4);
@@ -153,8 +163,9 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             for (int it = it_begin; list_ok && it < it_end && ok; ++it) {
                 const SharedItem item = p.items[it];
                 if (!shared_item_ok(item, p)) break;   // the other roles flag it and stop as well
+                const int tiles = item.mode == SHARED_TILES ? 2 : 1;
                 if (lane == 0) {
-                    for (int w = 0; w < item.tiles && ok; ++w) {
+                    for (int w = 0; w < tiles && ok; ++w) {
                         const uint32_t s = qs + w, slot = s & 1u;
                         if (s >= 2) ok = mbar_wait(&q_empty[slot], ((s >> 1) - 1) & 1u, p.status);
                         if (!ok) break;
@@ -163,7 +174,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                             tma_load_4d(qbuf + slot * SM::Q_BYTES + h * SM::Q_HALF, &tmQ, &q_full[slot], 0, h, item.kvh * G, item.q_tok + w * p.tile_tokens);
                     }
                 }
-                qs += item.tiles;
+                qs += tiles;
                 ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
                 if (!ok) break;
                 // page-table entries: the warp holds those of 4 stages (32 pages, one per lane) and fetches the next 32 meanwhile
@@ -188,7 +199,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll
                     for (int v = 0; v < 2; ++v) {
                         const uint32_t n = v ? VS : KS, s = st % n;
-                        uint64_t* full = (v ? v_full : k_full) + (item.tiles == 2 ? 2 : k & 1) * n;
+                        uint64_t* full = (v ? v_full : k_full) + (item.mode == SHARED_STAGES ? k & 1 : item.mode) * n;
                         if (lane == 0) {
                             if (st >= n) ok = mbar_wait(&(v ? v_empty : k_empty)[s], ((st / n) - 1) & 1u, p.status);
                             if (ok) mbar_expect_tx(&full[s], (uint32_t)npg * SM::BOX_BYTES);
@@ -213,8 +224,8 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             const uint64_t k_desc0 = umma_desc_k128s(smem_u32(kring), SM::GROUP_BYTES), v_desc0 = umma_desc_mn128(smem_u32(vring), 1024, SM::GROUP_BYTES);
             constexpr uint32_t SLOT16 = SM::K_BYTES >> 4, HALF16 = SLOT16 / 2;
             // P V's to come, at most two, the older first: pages | V slot << 4 | half << 8 | first << 9 | last << 10 | wait for V << 11 |
-            // its phase's parity << 12 | end of the stage << 13 | stage of both << 14; and the older one's stage
-            uint32_t todo0 = 0, todo1 = 0, stage0 = 0, stage1 = 0, n_todo = 0;
+            // its phase's parity << 12 | end of the stage << 13 | stage of both << 14
+            uint32_t todo0 = 0, todo1 = 0, n_todo = 0;
             uint32_t use = 0, o_use = 0;     // P V's so far, and items among them
             uint32_t st = 0, qs = 0;         // stage and Q slot of the item's first
             uint32_t k_own = 0, k_both = 0, v_own = 0, v_both = 0;   // bit s: parity of the next phase of slot s
@@ -222,7 +233,6 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             auto pv = [&]() {
                 const uint32_t f = todo0, pages = f & 15u, vs = (f >> 4) & 15u, buf = use & 1u;
                 todo0 = todo1;
-                stage0 = stage1;
                 --n_todo;
                 const bool first = (f >> 9) & 1u;
                 if ((f >> 11) & 1u) ok = mbar_wait(&v_full[((f >> 14) & 1u ? 2 : w) * VS + vs], (f >> 12) & 1u, p.status);
@@ -249,22 +259,23 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             for (int it = it_begin; list_ok && it < it_end && ok; ++it) {
                 const SharedItem item = p.items[it];
                 if (!shared_item_ok(item, p)) break;
-                const bool two = item.tiles == 2;
+                const bool two = item.mode == SHARED_TILES, both = item.mode == SHARED_STAGES;
+                const uint32_t tiles = two ? 2 : 1;
                 const int n_pages = (item.kv_end - item.kv_begin + 15) >> 4;
-                const uint32_t n_st = (uint32_t)(n_pages + SHR_PAGES - 1) / SHR_PAGES, step = two ? 1 : 2;
+                const uint32_t n_st = (uint32_t)(n_pages + SHR_PAGES - 1) / SHR_PAGES, step = both ? 2 : 1;
                 const uint64_t a = umma_desc_k128(smem_u32(qbuf + ((qs + (two ? w : 0)) & 1u) * SM::Q_BYTES));
-                // The producer requests K of stage s behind V of stage s - 1: no P V that holds a slot it needs may be pending when K (or
-                // Q) is waited for (one would be, of the second group, through any number of items of one stage).
-                while (ok && n_todo > 0 && (int)stage0 <= (int)st - VS) pv();
-                for (uint32_t q = qs; q < qs + item.tiles && ok; ++q) ok = mbar_wait(&q_full[q & 1u], (q >> 1) & 1u, p.status);
+                for (uint32_t q = qs; q < qs + tiles && ok; ++q) ok = mbar_wait(&q_full[q & 1u], (q >> 1) & 1u, p.status);
                 if (!ok) break;
                 uint32_t kb = two ? k_both : k_own, vb = two ? v_both : v_own;
-                if (!two && (uint32_t)w >= n_st) mbar_arrive(&q_empty[qs & 1u]);   // nothing here for the second group
-                uint32_t k = two ? 0 : w, ks = (st + k) % KS, vs = (st + k) % VS;
+                const bool none = !two && !both && item.mode != w;                 // the other group's
+                if (none) {
+                    mbar_arrive(&q_done[qs & 1u]);
+                    for (int i = 0; i < 4; ++i) mbar_arrive(&q_empty[qs & 1u]);
+                }
+                uint32_t k = none ? n_st : both ? w : 0, ks = (st + k) % KS, vs = (st + k) % VS;
                 for (; k < n_st && ok; k += step) {
-                    const uint32_t s = st + k, pages = (uint32_t)min(SHR_PAGES, n_pages - (int)k * SHR_PAGES);
-                    while (ok && n_todo > 0 && (int)stage0 <= (int)s - VS) pv();
-                    if (ok) ok = mbar_wait(&k_full[(two ? 2 : w) * KS + ks], (kb >> ks) & 1u, p.status);
+                    const uint32_t pages = (uint32_t)min(SHR_PAGES, n_pages - (int)k * SHR_PAGES);
+                    ok = mbar_wait(&k_full[(two ? 2 : w) * KS + ks], (kb >> ks) & 1u, p.status);
                     if (!ok) break;
                     const uint32_t v_parity = (vb >> vs) & 1u;
                     kb ^= 1u << ks;
@@ -289,15 +300,11 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                             if (!two) umma_commit(&k_empty[ks]);
                         }
                         if (last)
-                            for (uint32_t q = qs; q < qs + item.tiles; ++q) umma_commit(&q_empty[q & 1u]);
+                            for (uint32_t q = qs; q < qs + tiles; ++q) umma_commit(&q_done[q & 1u]);
                         const uint32_t f = here | vs << 4 | h << 8 | (uint32_t)first << 9 | (uint32_t)last << 10 | (uint32_t)(h == 0) << 11 | v_parity << 12 |
                                            (uint32_t)end << 13 | (uint32_t)two << 14;
-                        if (n_todo == 0) {
-                            todo0 = f;
-                            stage0 = s;
-                        }
+                        if (n_todo == 0) todo0 = f;
                         todo1 = f;
-                        stage1 = s;
                         ++n_todo;
                     }
                     ks += step;
@@ -307,10 +314,12 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 }
                 (two ? k_both : k_own) = kb;
                 (two ? v_both : v_own) = vb;
+                // The last P V's do not wait for the next item's turns: the group writes its results meanwhile, and the slots that they
+                // hold are needed before the producer, who works in order, can bring what those turns wait for.
+                while (ok && n_todo > 0) pv();
                 st += n_st;
-                qs += item.tiles;
+                qs += tiles;
             }
-            while (ok && n_todo > 0) pv();
         }
         __syncwarp();
     } else {
@@ -320,9 +329,10 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const int wg = (warp - 4) >> 2, wq = (warp - 4) & 3, row = wq * 32 + lane;   // group, lane quarter, row of the tile
         const uint32_t t_lane = tmem_base + ((uint32_t)(wq * 32) << 16);
         const uint32_t o_col = (uint32_t)wg * 128, s_col = 256 + (uint32_t)wg * 128;
-        uint32_t st = 0, use = 0, o_use = 0;
+        uint32_t st = 0, qs = 0, use = 0, o_use = 0;
         uint32_t v_own = 0, v_both = 0;   // as the issuer's
         bool ok = true;   // uniform over the warp: the tensor-memory loads and stores are warp-wide
+        if (wg == 1) shr_turn_over(wg, wq);
         auto wait_all = [&](uint64_t* bar, uint32_t parity) {
             const bool r = mbar_wait(bar, parity, p.status);
             return __all_sync(0xFFFFFFFFu, r) != 0;
@@ -333,7 +343,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 if (threadIdx.x == 128) atomicExch(p.status, 2);
                 break;
             }
-            const bool two = item.tiles == 2;
+            const bool two = item.mode == SHARED_TILES, both = item.mode == SHARED_STAGES;
             const int first_tok = two ? wg * p.tile_tokens : 0;       // of the group's tile, within the item
             const int rows = (two && wg == 0 ? p.tile_tokens : item.n_tok - first_tok) * G;
             const bool live = row < rows;
@@ -341,129 +351,166 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             const int n_st = (item.kv_end - item.kv_begin + SHARED_STAGE - 1) / SHARED_STAGE;
             const int lim = item.q_pos0 + first_tok + row / G;        // last visible key position of this row
             float m_used = -INFINITY, l = 0.f;
-            int mine = 0;                                             // half stages of this group
+            // The group's half stages: of every stage, or of every second one; the item's last stage may have one half.
+            const int first_k = both ? wg : 0, n_mine = both ? (n_st + 1 - wg) / 2 : two || item.mode == wg ? n_st : 0;
+            const int last_k = both ? first_k + 2 * (n_mine - 1) : n_st - 1;
+            const int mine = n_mine == 0 ? 0 : 2 * n_mine - (item.kv_end - item.kv_begin - last_k * SHARED_STAGE <= SHR_HALF ? 1 : 0);
+            auto stage_of = [&](int i) { return both ? first_k + (i & ~1) : i >> 1; };
+            auto key_of = [&](int i) { return item.kv_begin + stage_of(i) * SHARED_STAGE + (i & 1) * SHR_HALF; };
             const Two scale2 = two_of(p.scale_log2, p.scale_log2);
-            for (int k = 0; k < n_st; ++k) {
-                if (!two && (k & 1) != wg) continue;
-                const uint32_t vs = (uint32_t)(st + k) % VS, v_parity = ((two ? v_both : v_own) >> vs) & 1u;
-                (two ? v_both : v_own) ^= 1u << vs;
-                for (int kv0 = item.kv_begin + k * SHARED_STAGE, h = 0; h < 2 && kv0 < item.kv_end; ++h, kv0 += SHR_HALF, ++use, ++mine) {
-                    const uint32_t buf = use & 1u, s_tmem = t_lane + s_col + buf * 64;
-                    if (ok) ok = wait_all(&s_full[2 * wg + buf], (use >> 1) & 1u);
-                    if (wlive && ok) {
-                        uint32_t s[2][32];
-                        tc_fence_after();
-                        tmem_ld32(s_tmem, s[0]);
-                        tmem_ld32(s_tmem + 32, s[1]);
-                        tmem_ld_wait();
-                        // keys this row sees in the half stage: positions < min(kv_end, lim + 1)
-                        const int nvalid = min(item.kv_end, lim + 1) - kv0;
-                        if (nvalid < SHR_HALF) {
+            const int see = min(item.kv_end, lim + 1);                // the row sees keys below
+            // largest score of a half stage (log2 units), keys that the row does not see taken out
+            auto largest = [&](uint32_t (&s)[2][32], int i) {
+                const int nvalid = see - key_of(i);
+                if (nvalid < SHR_HALF) {
 #pragma unroll
-                            for (int c = 0; c < 2; ++c)
+                    for (int c = 0; c < 2; ++c)
 #pragma unroll
-                                for (int i = 0; i < 32; ++i)
-                                    if (32 * c + i >= nvalid) s[c][i] = 0xFF800000u;   // -inf
-                        }
-                        float mc[4];
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const uint32_t* x = &s[c >> 1][(c & 1) * 16];
-                            mc[c] = __uint_as_float(x[0]);
-#pragma unroll
-                            for (int i = 1; i < 15; i += 2) mc[c] = max3(mc[c], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
-                            mc[c] = fmaxf(mc[c], __uint_as_float(x[15]));
-                        }
-                        const float ms = fmaxf(max3(mc[0], mc[1], mc[2]), mc[3]) * p.scale_log2;
-                        if (mine == 0) {
-                            m_used = live ? ms : 0.f;
-                        } else {
-                            const bool grow = live && ms > m_used + ATT2_RESCALE_GAP;
-                            if (__any_sync(0xFFFFFFFFu, grow)) {
-                                // O is rescaled in tensor memory: the P V before must have completed.  (Those before it have: the scores
-                                // waited for above were issued behind them.  So this phase's parity is unmistakable.)
-                                ok = wait_all(&pv_done[wg], (use - 1) & 1u);
-                                const float corr = grow ? ex2_approx(m_used - ms) : 1.f;
-                                if (grow) {
-                                    m_used = ms;
-                                    l *= corr;
-                                }
-                                tc_fence_after();
-#pragma unroll 1
-                                for (int ch = 0; ok && ch < HD / 16; ++ch) {
-                                    uint32_t o[16];
-                                    tmem_ld16(t_lane + o_col + ch * 16, o);
-                                    tmem_ld_wait();
-#pragma unroll
-                                    for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * corr);
-                                    tmem_st16(t_lane + o_col + ch * 16, o);
-                                }
-                            }
-                        }
-                        const float base = (m_used == -INFINITY ? 0.f : m_used) - SHR_P_SCALE_LOG2;
-                        const Two base2 = two_of(-base, -base);
-                        Two sum[2] = {two_of(0.f, 0.f), two_of(0.f, 0.f)};
-                        uint32_t pw[2][16];
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                float a, b;
-                                untwo(fma2(two_of(__uint_as_float(s[c][2 * i]), __uint_as_float(s[c][2 * i + 1])), scale2, base2), a, b);
-                                a = ex2_approx(a);
-                                b = ex2_approx(b);
-                                sum[i & 1] = add2(sum[i & 1], two_of(a, b));
-                                pw[c][i] = pack_op(a, b);   // (rows beyond the tile's hold garbage: they only meet themselves in the products)
-                            }
-                            if (ok) tmem_st16(s_tmem + 16 * c, pw[c]);
-                        }
-                        float u0, u1;
-                        untwo(add2(sum[0], sum[1]), u0, u1);
-                        l += u0 + u1;
-                        tmem_st_wait();
-                        tc_fence_before();
-                    }
-                    // Rows of the last page behind the item's keys: a weight of zero takes whatever is stale there out, unless that is no
-                    // number.  Every group that uses the stage clears them before its P V can start.
-                    if ((item.kv_end & 15) && kv0 + SHR_HALF >= item.kv_end && ok) {
-                        // (the phase before is over: the issuer has seen it before this stage's scores)
-                        ok = wait_all(&v_full[(two ? 2 : wg) * VS + vs], v_parity);
-                        uint8_t* box = vring + vs * SM::K_BYTES + ((item.kv_end - 1 - item.kv_begin) / 16 - k * SHR_PAGES) * SM::BOX_BYTES;
-                        const int r0 = item.kv_end & 15;
-                        for (int c = row; ok && c < (16 - r0) * HALVES * 8; c += 128) {
-                            const int r = r0 + c / (HALVES * 8), half = (c >> 3) % HALVES;
-                            *reinterpret_cast<uint4*>(box + (r >> 3) * SM::GROUP_BYTES + half * 1024 + (r & 7) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
-                        }
-                        fence_proxy_async_smem();
-                    }
-                    __syncwarp();
-                    if (lane == 0 && ok) mbar_arrive(&p_full[2 * wg + buf]);
+                        for (int x = 0; x < 32; ++x)
+                            if (32 * c + x >= nvalid) s[c][x] = 0xFF800000u;   // -inf
                 }
+                float mc[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t* x = &s[c >> 1][(c & 1) * 16];
+                    mc[c] = __uint_as_float(x[0]);
+#pragma unroll
+                    for (int y = 1; y < 15; y += 2) mc[c] = max3(mc[c], __uint_as_float(x[y]), __uint_as_float(x[y + 1]));
+                    mc[c] = fmaxf(mc[c], __uint_as_float(x[15]));
+                }
+                return fmaxf(max3(mc[0], mc[1], mc[2]), mc[3]) * p.scale_log2;
+            };
+            for (int i = 0; i < mine; ++i, ++use) {
+                const uint32_t buf = use & 1u, s_tmem = t_lane + s_col + buf * 64;
+                if (ok) ok = wait_all(&s_full[2 * wg + buf], (use >> 1) & 1u);
+                uint32_t s[2][32];
+                const bool work = wlive && ok;
+                float base = 0.f;
+                if (work) {
+                    tc_fence_after();
+                    tmem_ld32(s_tmem, s[0]);
+                    tmem_ld32(s_tmem + 32, s[1]);
+                    tmem_ld_wait();
+                    const float ms = largest(s, i);
+                    if (i == 0) {
+                        m_used = live ? ms : 0.f;
+                    } else {
+                        const bool grow = live && ms > m_used + ATT2_RESCALE_GAP;
+                        if (__any_sync(0xFFFFFFFFu, grow)) {
+                            // O is rescaled in tensor memory: the P V before must have completed.  (Those before it have: these scores
+                            // were issued behind them.  So this phase's parity is unmistakable.)
+                            ok = wait_all(&pv_done[wg], (use - 1) & 1u);
+                            const float corr = grow ? ex2_approx(m_used - ms) : 1.f;
+                            if (grow) {
+                                m_used = ms;
+                                l *= corr;
+                            }
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int ch = 0; ok && ch < HD / 16; ++ch) {
+                                uint32_t o[16];
+                                tmem_ld16(t_lane + o_col + ch * 16, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * corr);
+                                tmem_st16(t_lane + o_col + ch * 16, o);
+                            }
+                        }
+                    }
+                    base = (m_used == -INFINITY ? 0.f : m_used) - SHR_P_SCALE_LOG2;
+                }
+                if (two) shr_turn(wg, wq);
+                if (work) {
+                    const Two base2 = two_of(-base, -base);
+                    Two sum[2] = {two_of(0.f, 0.f), two_of(0.f, 0.f)};
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t pw[16];
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) {
+                            float a, b;
+                            untwo(fma2(two_of(__uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1])), scale2, base2), a, b);
+                            a = ex2_approx(a);
+                            b = ex2_approx(b);
+                            sum[x & 1] = add2(sum[x & 1], two_of(a, b));
+                            pw[x] = pack_op(a, b);   // (rows beyond the tile's hold garbage: they only meet themselves in the products)
+                        }
+                        tmem_st16(s_tmem + 16 * c, pw);
+                    }
+                    float u0, u1;
+                    untwo(add2(sum[0], sum[1]), u0, u1);
+                    l += u0 + u1;
+                }
+                if (two) shr_turn_over(wg, wq);
+                if (work) {
+                    tmem_st_wait();
+                    tc_fence_before();
+                }
+                // Rows of the last page behind the item's keys: a weight of zero takes whatever is stale there out, unless that is no
+                // number.  Every group that uses the stage clears them before its P V can start.
+                const int k = stage_of(i);
+                const uint32_t vs = (uint32_t)(st + k) % VS, v_parity = ((two ? v_both : v_own) >> vs) & 1u;
+                if ((item.kv_end & 15) && i == mine - 1 && k == n_st - 1 && ok) {
+                    // (the phase before is over: the issuer has seen it before this stage's scores)
+                    ok = wait_all(&v_full[(two ? 2 : wg) * VS + vs], v_parity);
+                    uint8_t* box = vring + vs * SM::K_BYTES + ((item.kv_end - 1 - item.kv_begin) / 16 - k * SHR_PAGES) * SM::BOX_BYTES;
+                    const int r0 = item.kv_end & 15;
+                    for (int c = row; ok && c < (16 - r0) * HALVES * 8; c += 128) {
+                        const int r = r0 + c / (HALVES * 8), half = (c >> 3) % HALVES;
+                        *reinterpret_cast<uint4*>(box + (r >> 3) * SM::GROUP_BYTES + half * 1024 + (r & 7) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                }
+                if ((i & 1) || i == mine - 1) (two ? v_both : v_own) ^= 1u << vs;   // the stage is over
+                __syncwarp();
+                if (lane == 0 && ok) mbar_arrive(&p_full[2 * wg + buf]);
             }
             st += n_st;
-            if (mine == 0) continue;   // one tile, one stage: the second group has no part in it
-            // ---- end of the item: the fp32 partial (m, l, O) of the group's rows
+            const uint32_t q = qs + (two ? wg : 0);
+            qs += two ? 2 : 1;
+            if (mine == 0) continue;   // (the group's issuer has let the Q slot go)
+            // ---- end of the item: the fp32 partial (m, l, O) of the group's rows.  A row is a thread's in tensor memory; written
+            // like that, a store of 16 bytes would touch 32 lines a warp.  So the warp turns 32 rows x OUT_COLS columns at a time around in
+            // the Q slot, which the products no longer read.
             if (ok) ok = wait_all(&o_full[wg], o_use & 1u);
+            if (ok) ok = wait_all(&q_done[q & 1u], (q >> 1) & 1u);
             ++o_use;
             if (ok && wlive) {
+                constexpr int C = SM::OUT_COLS, CHUNKS = C / 4, PER = 32 / CHUNKS;   // 16-byte chunks of a row; rows of a store
                 tc_fence_after();
-                const int64_t at = (int64_t)item.base + (two ? first_tok * G : wg * item.n_tok * G) + row;
+                const int row0 = wq * 32;   // of the tile
+                float* out = p.part_o + ((int64_t)item.base + (two ? first_tok * G : both ? wg * item.n_tok * G : 0) + row0) * HD;
+                uint8_t* turn = qbuf + (q & 1u) * SM::Q_BYTES + (both ? wg * (SM::Q_BYTES / 2) : 0) + wq * (32 * C * 4);
+                const int r = lane / CHUNKS, c16 = lane % CHUNKS;
 #pragma unroll 1
-                for (int ch = 0; ch < HD / 32; ++ch) {
-                    uint32_t o[32];
-                    tmem_ld32(t_lane + o_col + ch * 32, o);
+                for (int ch = 0; ch < HD / C; ++ch) {
+                    uint32_t o[C];
+                    if constexpr (C == 32) tmem_ld32(t_lane + o_col + ch * C, o);
+                    else tmem_ld16(t_lane + o_col + ch * C, o);
                     tmem_ld_wait();
-                    if (live) {
-                        uint4* dst = reinterpret_cast<uint4*>(p.part_o + at * HD + ch * 32);
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) dst[c] = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                    for (int c = 0; c < CHUNKS; ++c)
+                        *reinterpret_cast<uint4*>(turn + lane * (C * 4) + ((c ^ (lane & (CHUNKS - 1))) << 4)) = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 32 / PER; ++i) {
+                        const int rr = i * PER + r;
+                        const uint4 v = *reinterpret_cast<const uint4*>(turn + rr * (C * 4) + ((c16 ^ (rr & (CHUNKS - 1))) << 4));
+                        if (row0 + rr < rows) *reinterpret_cast<uint4*>(out + (int64_t)rr * HD + ch * C + c16 * 4) = v;
                     }
+                    __syncwarp();
                 }
                 tc_fence_before();
-                if (live) p.part_ml[at] = make_float2((m_used == -INFINITY ? 0.f : m_used) - SHR_P_SCALE_LOG2, l);
+                if (live) p.part_ml[(int64_t)item.base + (two ? first_tok * G : both ? wg * item.n_tok * G : 0) + row] =
+                    make_float2((m_used == -INFINITY ? 0.f : m_used) - SHR_P_SCALE_LOG2, l);
+                fence_proxy_async_smem();
             }
             __syncwarp();
-            if (lane == 0 && ok) mbar_arrive(&o_empty[wg]);
+            if (lane == 0 && ok) {
+                mbar_arrive(&o_empty[wg]);
+                mbar_arrive(&q_empty[q & 1u]);
+                if (two) mbar_arrive(&q_empty[(q ^ 1u) & 1u]);
+            }
         }
     }
     // ---------------------------------------------------------------- teardown

@@ -23,13 +23,33 @@ struct SharedItem {
     int kv_begin, kv_end;    // keys (the first a multiple of 16)
     int q_pos0;              // token j sees keys <= q_pos0 + j
     int base;                // its first row of partial results: row (j, g) at base + j * G + g
-    int tiles;               // 2: two tiles, each over every stage; 1: one tile, two groups of warps over alternate stages, the second's
-                             // results n_tok * G rows behind the first's (if there is a second stage)
+    int mode;                // who works on it, SharedMode
     int pad0, pad1, pad2;
 };
 
-// Cycles of a stage, of an item, of a launch (see shared_plan).
-struct SharedCost { int stage1, stage2, item, fixed; };
+// The kernel has two groups of warps.  One tile of rows and few stages: the whole item is one group's, while the other has another
+// item.  One tile and many stages: the groups take alternate stages, and the second's partial results lie n_tok * G rows behind
+// the first's.  Two tiles: a tile each, over every stage.
+enum SharedMode { SHARED_GROUP0 = 0, SHARED_GROUP1 = 1, SHARED_TILES = 2, SHARED_STAGES = 3 };
+constexpr int SHARED_SOLO_STAGES = 4;    // most stages of an item that one group takes alone
+
+// Cycles of an item by its stages, and of a launch with its merge.
+struct SharedCost {
+    int tiles_stage, tiles_item;     // two tiles
+    int stages_stage, stages_item;   // one tile, both groups
+    int solo_stage, solo_item;       // one tile, one group; the other group's items run beside it
+    int fixed;
+    int64_t of(int tiles, int stages) const {
+        return tiles == 2 ? (int64_t)stages * tiles_stage + tiles_item
+                          : stages <= SHARED_SOLO_STAGES ? (int64_t)stages * solo_stage + solo_item : (int64_t)stages * stages_stage + stages_item;
+    }
+    // most stages whose item takes no more than `room`
+    int fit(int tiles, int64_t room) const {
+        if (tiles == 2) return (int)std::max<int64_t>(0, (room - tiles_item) / tiles_stage);
+        const int64_t n = (room - stages_item) / stages_stage;
+        return n > SHARED_SOLO_STAGES ? (int)n : (int)std::min<int64_t>(SHARED_SOLO_STAGES, std::max<int64_t>(0, (room - solo_item) / solo_stage));
+    }
+};
 
 struct SharedPlan {
     bool shares = false;                 // some keys are met by several requests' tokens
@@ -87,7 +107,7 @@ inline void shared_plan(int n_req, const int* chunk_offsets, const int* page_tab
     const std::vector<SharedNode> nodes = shared_tree(n_req, page_tables, max_pages, ctx_lens, page_size, SHARED_STAGE / page_size);
     const int T = chunk_offsets[n_req], tile_tokens = SHARED_TILE_ROWS / group;
     // units: a node's tokens in items of at most two tiles
-    struct Unit { int q_tok, n_tok, req, kv_begin, kv_end, q_pos0, tiles, stages; int64_t stage; };
+    struct Unit { int q_tok, n_tok, req, kv_begin, kv_end, q_pos0, tiles, stages; int64_t time; };
     std::vector<Unit> units;
     std::vector<int> cuts = {0, T};
     for (const SharedNode& nd : nodes) {
@@ -101,17 +121,17 @@ inline void shared_plan(int n_req, const int* chunk_offsets, const int* page_tab
             // a leaf's tokens see keys up to their own position; those of its first tiles need not read what only later ones see
             const int end = leaf ? ctx_lens[nd.a] + (t - t0) + n : kv1;
             Unit u = {t, n, nd.a, kv0, end, leaf ? ctx_lens[nd.a] + (t - t0) : SHARED_NO_LIMIT, n > tile_tokens ? 2 : 1, (end - kv0 + SHARED_STAGE - 1) / SHARED_STAGE, 0};
-            u.stage = u.tiles == 2 ? cost.stage2 : cost.stage1;
+            u.time = cost.of(u.tiles, u.stages);
             units.push_back(u);
             cuts.push_back(t);
             cuts.push_back(t + n);
         }
     }
-    std::stable_sort(units.begin(), units.end(), [](const Unit& x, const Unit& y) { return x.stages * x.stage > y.stages * y.stage; });
+    std::stable_sort(units.begin(), units.end(), [](const Unit& x, const Unit& y) { return x.time > y.time; });
     int64_t total = 0, longest = 0;
     for (const Unit& u : units) {
-        total += (u.stages * u.stage + cost.item) * n_kv_heads;
-        longest = std::max(longest, u.stages * u.stage + cost.item);
+        total += u.time * n_kv_heads;
+        longest = std::max(longest, u.time);
     }
     // The units one after the other, longest first, each CTA filled up to `limit`; what does not fit goes on in the next CTA.
     auto fill = [&](int64_t limit, auto&& emit) {
@@ -120,13 +140,12 @@ inline void shared_plan(int n_req, const int* chunk_offsets, const int* page_tab
         for (const Unit& u : units)
             for (int h = 0; h < n_kv_heads; ++h)
                 for (int at = 0; at < u.stages;) {
-                    const int64_t room = (limit - load - cost.item) / u.stage;
-                    int take = (int)std::min<int64_t>(u.stages - at, std::max<int64_t>(room, 0));
+                    int take = std::min(u.stages - at, cost.fit(u.tiles, limit - load));
                     if (take < u.stages - at && take < 2) take = 0;      // no slivers
                     if (take == 0 && load == 0) return false;
                     if (take) {
                         emit(u, h, at, at + take, cta);
-                        load += take * u.stage + cost.item;
+                        load += cost.of(u.tiles, take);
                         at += take;
                     }
                     if (at < u.stages) {
@@ -144,14 +163,15 @@ inline void shared_plan(int n_req, const int* chunk_offsets, const int* page_tab
         if (fill(mid, nothing)) hi = mid; else lo = mid;
     }
     sp.estimate = hi + cost.fixed;
-    std::vector<int> owner;
+    std::vector<int> owner, solo(n_sm, 0);   // (a CTA's items of one group: the groups in turn)
     // parts of (unit, head), for the lists below
     struct Part { int unit, h, base, second; };
     std::vector<Part> parts;
     fill(hi, [&](const Unit& u, int h, int s0, int s1, int cta) {
-        const int rows = u.n_tok * group, copies = u.tiles == 1 && s1 - s0 > 1 ? 2 : 1;
+        const int mode = u.tiles == 2 ? SHARED_TILES : s1 - s0 > SHARED_SOLO_STAGES ? SHARED_STAGES : solo[cta]++ & 1;
+        const int rows = u.n_tok * group, copies = mode == SHARED_STAGES ? 2 : 1;
         sp.items.push_back({u.q_tok, u.n_tok, h, u.req, u.kv_begin + s0 * SHARED_STAGE, std::min(u.kv_end, u.kv_begin + s1 * SHARED_STAGE), u.q_pos0,
-                            (int)sp.rows, u.tiles, 0, 0, 0});
+                            (int)sp.rows, mode, 0, 0, 0});
         parts.push_back({(int)(&u - units.data()), h, (int)sp.rows, copies == 2 ? (int)sp.rows + rows : -1});
         sp.rows += (int64_t)rows * copies;
         owner.push_back(cta);

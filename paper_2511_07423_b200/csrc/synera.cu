@@ -1258,9 +1258,9 @@ static int plan_compute(const syn_model_desc& c, int P, uint32_t n_pages, int n_
 // The attention kernel that plans are laid out for unless they share prefixes (0: the planner's choice).
 static int attention_choice() { return g_attention == ATTN_SHARED ? 0 : g_attention; }
 
-// SM cycles of the shared-prefix kernel: a stage of 128 keys with one tile of rows and with two, an item, a launch with its merge.
+// SM cycles of the shared-prefix kernel, fitted to the items' own times in the batches of the 8B and 32B shapes.
 static SharedCost shared_cost(const syn_model_desc& c) {
-    return c.head_dim == 128 ? SharedCost{2400, 3600, 4000, 14000} : SharedCost{1600, 2600, 4000, 14000};
+    return c.head_dim == 128 ? SharedCost{3450, 11000, 2700, 4000, 1400, 6000, 14000} : SharedCost{2600, 9000, 2000, 4000, 1100, 5000, 14000};
 }
 
 // Whether a batch planned as `hp` is better off with its common prefixes met once; fills `sp`.
@@ -1478,7 +1478,7 @@ static int syn_plan_shared_host_impl(const syn_model_desc* desc, uint32_t n_page
         for (int i = 0; i < *n_items; ++i) {
             const SharedItem& it = sp.items[i];
             const int32_t row[SYN_SHARED_ITEM_FIELDS] = {it.q_tok, it.n_tok, it.kvh, it.req, it.kv_begin, it.kv_end,
-                                                         it.q_pos0 == SHARED_NO_LIMIT ? -1 : it.q_pos0, it.base, it.tiles};
+                                                         it.q_pos0 == SHARED_NO_LIMIT ? -1 : it.q_pos0, it.base, it.mode};
             memcpy(items + (size_t)i * SYN_SHARED_ITEM_FIELDS, row, sizeof(row));
         }
     if (cta_begin) memcpy(cta_begin, sp.cta_begin.data(), (size_t)(sp.n_cta + 1) * 4);

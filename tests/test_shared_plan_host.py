@@ -59,7 +59,7 @@ def test_every_token_meets_its_keys_once(case):
     table, ctx, off, n_pages = tree_batch(rng, own, chunk, levels)
     T, G = int(off[-1]), hq // hkv
     p = syn.plan_shared_host(shape(hd, hq, hkv), n_pages, torch.zeros(T, dtype=torch.int32), off, table, ctx, n_sm=n_sm)
-    items = [dict(zip(("q_tok", "n_tok", "kvh", "req", "kv_begin", "kv_end", "q_pos0", "base", "tiles"), r)) for r in p["items"].tolist()]
+    items = [dict(zip(("q_tok", "n_tok", "kvh", "req", "kv_begin", "kv_end", "q_pos0", "base", "mode"), r)) for r in p["items"].tolist()]
     assert p["n_cta"] <= n_sm and p["cta_begin"].tolist()[0] == 0 and p["cta_begin"].tolist()[-1] == len(items)
     assert all(a < b for a, b in zip(p["cta_begin"].tolist(), p["cta_begin"].tolist()[1:]))
     req_of = [i for i in range(len(own)) for _ in range(chunk[i])]
@@ -69,10 +69,12 @@ def test_every_token_meets_its_keys_once(case):
     used = set()
     tile = 128 // G
     for it in items:
-        assert 1 <= it["n_tok"] <= tile * it["tiles"] and it["tiles"] in (1, 2) and (it["tiles"] == 1 or it["n_tok"] > tile)
+        tiles = 2 if it["mode"] == 2 else 1
+        assert 1 <= it["n_tok"] <= tile * tiles and it["mode"] in (0, 1, 2, 3) and (tiles == 1 or it["n_tok"] > tile)
         assert it["kv_begin"] % 16 == 0 and it["kv_begin"] < it["kv_end"]
         stages = -(-(it["kv_end"] - it["kv_begin"]) // STAGE)
-        copies = 2 if it["tiles"] == 1 and stages > 1 else 1
+        copies = 2 if it["mode"] == 3 else 1
+        assert copies == 1 or stages > 1
         span = range(it["base"], it["base"] + copies * it["n_tok"] * G)
         assert not used & set(span)
         used |= set(span)
@@ -149,7 +151,7 @@ def test_many_requests_in_a_chain_of_prefixes():
     off = torch.arange(n + 1, dtype=torch.int32)
     p = syn.plan_shared_host(shape(64, 8, 2), at + n, torch.zeros(n, dtype=torch.int32), off, table, torch.tensor(ctx, dtype=torch.int32))
     keys = {}
-    for q_tok, n_tok, h, req, b, e, q0, base, tiles in p["items"].tolist():
+    for q_tok, n_tok, h, req, b, e, q0, base, mode in p["items"].tolist():
         for t in range(q_tok, q_tok + n_tok):
             if h == 0:
                 keys[t] = keys.get(t, 0) + (e - b if q0 < 0 else min(e, ctx[t] + 1) - b)
