@@ -6,7 +6,7 @@
 //   out = sum_k 2^(m_k - m) O_k / sum_k 2^(m_k - m) l_k,  m = max_k m_k.
 // Both products run on tcgen05.mma with M = 128, in stages of 128 keys (8 pages):
 //   S = Q K^T : A = a Q tile, B = the stage's K, D = S in tensor memory (128 columns a tile);
-//   O += P V  : A = P in half precision in tensor memory, over the first 64 columns of S, B = V as it lies in the cache, D = O.
+//   O += P V  : A = P in half precision in tensor memory, B = V as it lies in the cache, D = O.
 // P in tensor memory leaves shared memory's bandwidth to the operands: with both of a product's operands there, a k-step of 64
 // cycles reads 8 KB, all that 128 bytes a cycle can deliver.
 // Two groups of four softmax warps (thread = row), each with its own S, P and O.  With two tiles a group owns a tile and takes
@@ -69,7 +69,7 @@ struct SharedSmem {
     static constexpr int K_SLOTS = HD == 128 ? 2 : 5, V_SLOTS = HD == 128 ? 3 : 6;
     static constexpr int TOTAL = 1024 + 2 * Q_BYTES + (K_SLOTS + V_SLOTS) * K_BYTES + SHR_BAR_BYTES;
     static_assert(TOTAL <= 232448, "shared memory of one CTA");
-    static constexpr int TMEM_COLS = 512;   // O of the two groups at 0 and 128; S (and P) at 256 and 384
+    static constexpr int TMEM_COLS = 512;   // O of the two groups at 0 and 128; S and P at 256 and 384
 };
 
 // D[tmem] (+)= A[tmem] * B[smem]; one thread issues.
@@ -108,13 +108,14 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     uint64_t* q_full = v_empty + VS;     // [slot]
     uint64_t* q_done = q_full + 2;       // [slot] the last Q K^T that reads it is complete
     uint64_t* q_empty = q_done + 2;      // [slot] nor do the softmax warps use it any more
-    uint64_t* s_full = q_empty + 2;      // [group][buffer] scores of a half stage (and what was issued before them) are complete
-    uint64_t* p_full = s_full + 4;       // [group][buffer] P of a half stage is in tensor memory (and O rescaled if need be)
-    uint64_t* pv_done = p_full + 4;      // [group] a P V is complete
-    uint64_t* o_full = pv_done + 2;      // [group] the item's last P V is complete
+    uint64_t* s_full = q_empty + 2;      // [group] scores of a half stage are complete
+    uint64_t* s_empty = s_full + 2;      // [group] its warps hold them in registers
+    uint64_t* p_full = s_empty + 2;      // [group][buffer] P of a half stage is in tensor memory (and O rescaled if need be)
+    uint64_t* pv_done = p_full + 4;      // [group][buffer] its P V is complete
+    uint64_t* o_full = pv_done + 4;      // [group] the item's last P V is complete
     uint64_t* o_empty = o_full + 2;      // [group] its warps have read O
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_empty + 2);
-    static_assert((4 * KS + 4 * VS + 20) * 8 + 4 <= SHR_BAR_BYTES, "barrier area");
+    static_assert((4 * KS + 4 * VS + 22) * 8 + 4 <= SHR_BAR_BYTES, "barrier area");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int it_begin = p.cta_begin[blockIdx.x], it_end = p.cta_begin[blockIdx.x + 1];
@@ -132,11 +133,12 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             mbar_init(&q_full[s], 1);
             mbar_init(&q_done[s], 2);
             mbar_init(&q_empty[s], 8);
+            mbar_init(&s_full[s], 1);
+            mbar_init(&s_empty[s], 4);
             for (int b = 0; b < 2; ++b) {
-                mbar_init(&s_full[2 * s + b], 1);
                 mbar_init(&p_full[2 * s + b], 4);
+                mbar_init(&pv_done[2 * s + b], 1);
             }
-            mbar_init(&pv_done[s], 1);
             mbar_init(&o_full[s], 1);
             mbar_init(&o_empty[s], 4);
         }
@@ -214,38 +216,37 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             }
         } else if ((warp == SHR_MMA_WARP0 || warp == SHR_MMA_WARP0 + 1) && elect_one()) {
             // -------------------------------------------------------- MMA issuers, one a group
-            // A group works through half stages of 64 keys with two score buffers: the scores of half u + 1 are there while it
-            // computes the weights of half u.  Its issuer's turn: P V of half u - 2, then Q K^T of half u into the buffer that this
-            // P V has read (operations of one thread complete in order).  One thread for both groups was the bound: a turn takes it
-            // about 1 200 cycles, the group's weights of a half stage 1 100.
+            // A group works through half stages of 64 keys with one buffer of scores and two of P: as soon as its warps hold the
+            // scores of half u in registers, those of half u + 1 are computed, beside its exponentials; P V of half u follows.  (P
+            // over its own scores, in two buffers of these: the way P V, Q K^T, next scores was longer than a half stage's
+            // exponentials; 3 450 cycles a stage.  One issuer for both groups: 1 200 cycles a turn, 5 000 a stage.)
             const int w = warp - SHR_MMA_WARP0;
             const uint32_t idesc_pv = umma_idesc_f16_bmn(128, HD), idesc_qk = umma_idesc_f16(128, SHR_HALF);
-            const uint32_t o_tmem = tmem_base + w * 128, s_tmem0 = tmem_base + 256 + w * 128;
+            const uint32_t o_tmem = tmem_base + w * 128, s_tmem = tmem_base + 256 + w * 128;
             const uint64_t k_desc0 = umma_desc_k128s(smem_u32(kring), SM::GROUP_BYTES), v_desc0 = umma_desc_mn128(smem_u32(vring), 1024, SM::GROUP_BYTES);
             constexpr uint32_t SLOT16 = SM::K_BYTES >> 4, HALF16 = SLOT16 / 2;
-            // P V's to come, at most two, the older first: pages | V slot << 4 | half << 8 | first << 9 | last << 10 | wait for V << 11 |
-            // its phase's parity << 12 | end of the stage << 13 | stage of both << 14
-            uint32_t todo0 = 0, todo1 = 0, n_todo = 0;
+            // the P V to come: pages | V slot << 4 | half << 8 | first << 9 | last << 10 | wait for V << 11 | its phase's parity << 12 |
+            // end of the stage << 13 | stage of both << 14; 0: none
+            uint32_t todo = 0;
             uint32_t use = 0, o_use = 0;     // P V's so far, and items among them
             uint32_t st = 0, qs = 0;         // stage and Q slot of the item's first
             uint32_t k_own = 0, k_both = 0, v_own = 0, v_both = 0;   // bit s: parity of the next phase of slot s
             bool ok = true;
             auto pv = [&]() {
-                const uint32_t f = todo0, pages = f & 15u, vs = (f >> 4) & 15u, buf = use & 1u;
-                todo0 = todo1;
-                --n_todo;
+                const uint32_t f = todo, pages = f & 15u, vs = (f >> 4) & 15u, buf = use & 1u;
+                todo = 0;
                 const bool first = (f >> 9) & 1u;
                 if ((f >> 11) & 1u) ok = mbar_wait(&v_full[((f >> 14) & 1u ? 2 : w) * VS + vs], (f >> 12) & 1u, p.status);
                 if (ok && first && o_use > 0) ok = mbar_wait(&o_empty[w], (o_use - 1) & 1u, p.status);
                 if (ok) ok = mbar_wait(&p_full[2 * w + buf], (use >> 1) & 1u, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                const uint32_t p_tmem = s_tmem0 + buf * 64;
+                const uint32_t p_tmem = s_tmem + 64 + buf * 32;
                 const uint64_t b = v_desc0 + vs * SLOT16 + ((f >> 8) & 1u) * HALF16;
 #pragma unroll
                 for (uint32_t i = 0; i < SHR_PAGES / 2; ++i)   // step i: the 16 keys of a page; an item's first P V starts its O afresh
                     if (i < pages) umma_f16_ta(o_tmem, p_tmem + 8 * i, b + i * (SM::BOX_BYTES >> 4), idesc_pv, !first || i != 0);
-                umma_commit(&pv_done[w]);
+                umma_commit(&pv_done[2 * w + buf]);
                 if ((f >> 13) & 1u) {
                     umma_commit(&v_empty[vs]);
                     if (!((f >> 14) & 1u)) umma_commit(&v_empty[vs]);
@@ -275,7 +276,9 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 uint32_t k = none ? n_st : both ? w : 0, ks = (st + k) % KS, vs = (st + k) % VS;
                 for (; k < n_st && ok; k += step) {
                     const uint32_t pages = (uint32_t)min(SHR_PAGES, n_pages - (int)k * SHR_PAGES);
-                    ok = mbar_wait(&k_full[(two ? 2 : w) * KS + ks], (kb >> ks) & 1u, p.status);
+                    uint64_t* kf = &k_full[(two ? 2 : w) * KS + ks];
+                    if (todo && !mbar_test(kf, (kb >> ks) & 1u)) pv();      // K is not there yet: P V need not wait for it
+                    if (ok) ok = mbar_wait(kf, (kb >> ks) & 1u, p.status);
                     if (!ok) break;
                     const uint32_t v_parity = (vb >> vs) & 1u;
                     kb ^= 1u << ks;
@@ -283,17 +286,17 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll
                     for (uint32_t h = 0; h < 2; ++h) {
                         if (!ok || h * (SHR_PAGES / 2) >= pages) continue;
-                        if (n_todo == 2) pv();
+                        const uint32_t u = use + (todo != 0);               // half stages of the group before this one
+                        if (u > 0) ok = mbar_wait(&s_empty[w], (u - 1) & 1u, p.status);
                         if (!ok) continue;
                         tc_fence_after();
-                        const uint32_t here = min((uint32_t)SHR_PAGES / 2, pages - h * (SHR_PAGES / 2)), buf = (use + n_todo) & 1u;
-                        const uint32_t s_tmem = s_tmem0 + buf * 64;
+                        const uint32_t here = min((uint32_t)SHR_PAGES / 2, pages - h * (SHR_PAGES / 2));
                         const uint64_t b = k_desc0 + ks * SLOT16 + h * HALF16;
                         const uint32_t idesc = here == SHR_PAGES / 2 ? idesc_qk : umma_idesc_f16(128, 16 * here);
 #pragma unroll
                         for (uint32_t i = 0; i < HD / 16; ++i)   // step i: 16 dims, of the second half from step 4 on
                             umma_bf16(s_tmem, a + (i >> 2) * (SM::Q_HALF >> 4) + 2 * (i & 3), b + (i >> 2) * (1024 >> 4) + 2 * (i & 3), idesc, i != 0);
-                        umma_commit(&s_full[2 * w + buf]);
+                        umma_commit(&s_full[w]);
                         const bool end = (h + 1) * (SHR_PAGES / 2) >= pages, first = k < step && h == 0, last = k + step >= n_st && end;
                         if (end) {
                             umma_commit(&k_empty[ks]);
@@ -301,11 +304,9 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                         }
                         if (last)
                             for (uint32_t q = qs; q < qs + tiles; ++q) umma_commit(&q_done[q & 1u]);
-                        const uint32_t f = here | vs << 4 | h << 8 | (uint32_t)first << 9 | (uint32_t)last << 10 | (uint32_t)(h == 0) << 11 | v_parity << 12 |
-                                           (uint32_t)end << 13 | (uint32_t)two << 14;
-                        if (n_todo == 0) todo0 = f;
-                        todo1 = f;
-                        ++n_todo;
+                        if (todo) pv();
+                        todo = here | vs << 4 | h << 8 | (uint32_t)first << 9 | (uint32_t)last << 10 | (uint32_t)(h == 0) << 11 | v_parity << 12 |
+                               (uint32_t)end << 13 | (uint32_t)two << 14;
                     }
                     ks += step;
                     if (ks >= (uint32_t)KS) ks -= KS;
@@ -314,9 +315,9 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 }
                 (two ? k_both : k_own) = kb;
                 (two ? v_both : v_own) = vb;
-                // The last P V's do not wait for the next item's turns: the group writes its results meanwhile, and the slots that they
-                // hold are needed before the producer, who works in order, can bring what those turns wait for.
-                while (ok && n_todo > 0) pv();
+                // The last P V does not wait for the next item's scores: the group writes its results meanwhile, and the slots that it
+                // holds are needed before the producer, who works in order, can bring what those wait for.
+                if (ok && todo) pv();
                 st += n_st;
                 qs += tiles;
             }
@@ -329,14 +330,16 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         const int wg = (warp - 4) >> 2, wq = (warp - 4) & 3, row = wq * 32 + lane;   // group, lane quarter, row of the tile
         const uint32_t t_lane = tmem_base + ((uint32_t)(wq * 32) << 16);
         const uint32_t o_col = (uint32_t)wg * 128, s_col = 256 + (uint32_t)wg * 128;
-        uint32_t st = 0, qs = 0, use = 0, o_use = 0;
+        uint32_t qs = 0, use = 0, o_use = 0;
         uint32_t v_own = 0, v_both = 0;   // as the issuer's
         bool ok = true;   // uniform over the warp: the tensor-memory loads and stores are warp-wide
         if (wg == 1) shr_turn_over(wg, wq);
         auto wait_all = [&](uint64_t* bar, uint32_t parity) {
+            if (__all_sync(0xFFFFFFFFu, mbar_test(bar, parity))) return true;
             const bool r = mbar_wait(bar, parity, p.status);
             return __all_sync(0xFFFFFFFFu, r) != 0;
         };
+        uint32_t vs = 0;                  // V slot of the item's first stage
         for (int it = it_begin; list_ok && it < it_end; ++it) {
             const SharedItem item = p.items[it];
             if (!shared_item_ok(item, p)) {   // uniform over the CTA
@@ -355,13 +358,11 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             const int first_k = both ? wg : 0, n_mine = both ? (n_st + 1 - wg) / 2 : two || item.mode == wg ? n_st : 0;
             const int last_k = both ? first_k + 2 * (n_mine - 1) : n_st - 1;
             const int mine = n_mine == 0 ? 0 : 2 * n_mine - (item.kv_end - item.kv_begin - last_k * SHARED_STAGE <= SHR_HALF ? 1 : 0);
-            auto stage_of = [&](int i) { return both ? first_k + (i & ~1) : i >> 1; };
-            auto key_of = [&](int i) { return item.kv_begin + stage_of(i) * SHARED_STAGE + (i & 1) * SHR_HALF; };
             const Two scale2 = two_of(p.scale_log2, p.scale_log2);
             const int see = min(item.kv_end, lim + 1);                // the row sees keys below
             // largest score of a half stage (log2 units), keys that the row does not see taken out
-            auto largest = [&](uint32_t (&s)[2][32], int i) {
-                const int nvalid = see - key_of(i);
+            auto largest = [&](uint32_t (&s)[2][32], int kv0) {
+                const int nvalid = see - kv0;
                 if (nvalid < SHR_HALF) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
@@ -380,9 +381,11 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 }
                 return fmaxf(max3(mc[0], mc[1], mc[2]), mc[3]) * p.scale_log2;
             };
-            for (int i = 0; i < mine; ++i, ++use) {
-                const uint32_t buf = use & 1u, s_tmem = t_lane + s_col + buf * 64;
-                if (ok) ok = wait_all(&s_full[2 * wg + buf], (use >> 1) & 1u);
+            const int step = both ? 2 : 1;
+            int kv0 = item.kv_begin + first_k * SHARED_STAGE;
+            for (int i = 0; i < mine; ++i, ++use, kv0 += (i & 1) ? SHR_HALF : SHR_HALF + (step - 1) * SHARED_STAGE) {
+                const uint32_t buf = use & 1u, s_tmem = t_lane + s_col, p_tmem = s_tmem + 64 + buf * 32;
+                if (ok) ok = wait_all(&s_full[wg], use & 1u);
                 uint32_t s[2][32];
                 const bool work = wlive && ok;
                 float base = 0.f;
@@ -391,15 +394,20 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                     tmem_ld32(s_tmem, s[0]);
                     tmem_ld32(s_tmem + 32, s[1]);
                     tmem_ld_wait();
-                    const float ms = largest(s, i);
+                    tc_fence_before();
+                }
+                __syncwarp();
+                if (lane == 0 && ok) mbar_arrive(&s_empty[wg]);
+                if (work) {
+                    const float ms = largest(s, kv0);
                     if (i == 0) {
                         m_used = live ? ms : 0.f;
                     } else {
                         const bool grow = live && ms > m_used + ATT2_RESCALE_GAP;
                         if (__any_sync(0xFFFFFFFFu, grow)) {
-                            // O is rescaled in tensor memory: the P V before must have completed.  (Those before it have: these scores
-                            // were issued behind them.  So this phase's parity is unmistakable.)
-                            ok = wait_all(&pv_done[wg], (use - 1) & 1u);
+                            // O is rescaled in tensor memory: the P V before must have completed.  (The one before that has, and with
+                            // it P's buffer is free: these scores were issued behind it.)
+                            ok = wait_all(&pv_done[2 * wg + (buf ^ 1u)], ((use - 1) >> 1) & 1u);
                             const float corr = grow ? ex2_approx(m_used - ms) : 1.f;
                             if (grow) {
                                 m_used = ms;
@@ -435,7 +443,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                             sum[x & 1] = add2(sum[x & 1], two_of(a, b));
                             pw[x] = pack_op(a, b);   // (rows beyond the tile's hold garbage: they only meet themselves in the products)
                         }
-                        tmem_st16(s_tmem + 16 * c, pw);
+                        tmem_st16(p_tmem + 16 * c, pw);
                     }
                     float u0, u1;
                     untwo(add2(sum[0], sum[1]), u0, u1);
@@ -448,24 +456,33 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 }
                 // Rows of the last page behind the item's keys: a weight of zero takes whatever is stale there out, unless that is no
                 // number.  Every group that uses the stage clears them before its P V can start.
-                const int k = stage_of(i);
-                const uint32_t vs = (uint32_t)(st + k) % VS, v_parity = ((two ? v_both : v_own) >> vs) & 1u;
-                if ((item.kv_end & 15) && i == mine - 1 && k == n_st - 1 && ok) {
-                    // (the phase before is over: the issuer has seen it before this stage's scores)
-                    ok = wait_all(&v_full[(two ? 2 : wg) * VS + vs], v_parity);
-                    uint8_t* box = vring + vs * SM::K_BYTES + ((item.kv_end - 1 - item.kv_begin) / 16 - k * SHR_PAGES) * SM::BOX_BYTES;
-                    const int r0 = item.kv_end & 15;
-                    for (int c = row; ok && c < (16 - r0) * HALVES * 8; c += 128) {
-                        const int r = r0 + c / (HALVES * 8), half = (c >> 3) % HALVES;
-                        *reinterpret_cast<uint4*>(box + (r >> 3) * SM::GROUP_BYTES + half * 1024 + (r & 7) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                if (i == mine - 1) {
+                    // the V slots of the group's stages: their phases turn over
+                    uint32_t& v_bits = two ? v_both : v_own;
+                    uint32_t slot = (vs + (uint32_t)first_k) % VS;
+                    for (int n = 1; n < n_mine; ++n) {
+                        v_bits ^= 1u << slot;
+                        slot += step;
+                        if (slot >= (uint32_t)VS) slot -= VS;
                     }
-                    fence_proxy_async_smem();
+                    const uint32_t parity = (v_bits >> slot) & 1u;
+                    v_bits ^= 1u << slot;
+                    if ((item.kv_end & 15) && last_k == n_st - 1 && ok) {
+                        // (the phase before is over: the issuer has seen it before this stage's scores)
+                        ok = wait_all(&v_full[(two ? 2 : wg) * VS + slot], parity);
+                        uint8_t* box = vring + slot * SM::K_BYTES + ((item.kv_end - 1 - item.kv_begin) / 16 - last_k * SHR_PAGES) * SM::BOX_BYTES;
+                        const int r0 = item.kv_end & 15;
+                        for (int c = row; ok && c < (16 - r0) * HALVES * 8; c += 128) {
+                            const int r = r0 + c / (HALVES * 8), half = (c >> 3) % HALVES;
+                            *reinterpret_cast<uint4*>(box + (r >> 3) * SM::GROUP_BYTES + half * 1024 + (r & 7) * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_proxy_async_smem();
+                    }
                 }
-                if ((i & 1) || i == mine - 1) (two ? v_both : v_own) ^= 1u << vs;   // the stage is over
                 __syncwarp();
                 if (lane == 0 && ok) mbar_arrive(&p_full[2 * wg + buf]);
             }
-            st += n_st;
+            vs = (vs + (uint32_t)n_st) % VS;
             const uint32_t q = qs + (two ? wg : 0);
             qs += two ? 2 : 1;
             if (mine == 0) continue;   // (the group's issuer has let the Q slot go)

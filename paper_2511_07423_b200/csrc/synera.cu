@@ -1260,7 +1260,7 @@ static int attention_choice() { return g_attention == ATTN_SHARED ? 0 : g_attent
 
 // SM cycles of the shared-prefix kernel, fitted to the items' own times in the batches of the 8B and 32B shapes.
 static SharedCost shared_cost(const syn_model_desc& c) {
-    return c.head_dim == 128 ? SharedCost{3450, 11000, 2700, 4000, 1400, 6000, 14000} : SharedCost{2600, 9000, 2000, 4000, 1100, 5000, 14000};
+    return c.head_dim == 128 ? SharedCost{3450, 11500, 2550, 4500, 1900, 3600, 14000} : SharedCost{2600, 9000, 2000, 4000, 1100, 5000, 14000};
 }
 
 // Whether a batch planned as `hp` is better off with its common prefixes met once; fills `sp`.
