@@ -539,36 +539,60 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     }
 }
 
-// Joins the partials of a (token, query head), one warp each: the lanes read 32 parts' (m, l) at a time, then O part by part.
-template <int HD>
-__global__ void __launch_bounds__(128)
+// Joins the partials of a (token, query head): WPR warps take its parts in turn.  The lanes of a warp read 32 parts' (m, l) at a
+// time, then O part by part, four on their way at once (eight where a block has one row: there the parts are many and the warps few).  Which rows belong together is the plan's, so it is looked up before
+// the predecessor's results are waited for.
+constexpr int SHR_MERGE_SPLIT_ROWS = 16;   // rows an SM from which on a warp takes one alone
+template <int HD, int WPR>
+__global__ void __launch_bounds__(128, WPR > 1 ? 1 : 12)
 shared_merge_kernel(SharedParams p, int n_rows_out) {
     constexpr int E = HD / 32;   // components of a lane
-    const int r = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    __shared__ float part[WPR > 1 ? 4 : 1][WPR > 1 ? HD + 2 : 1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int r = WPR > 1 ? blockIdx.x : blockIdx.x * 4 + warp, w0 = WPR > 1 ? warp : 0;
     pdl_launch_dependents();
+    int t = 0, hq = 0, off = 0, b = 0, e = 0;
+    if (r < n_rows_out) {
+        const int n_q_heads = p.n_kv_heads * p.group;
+        t = r / n_q_heads;
+        hq = r - t * n_q_heads;
+        const int kvh = hq / p.group, seg = p.seg_of_token[t];
+        off = (t - p.seg_first[seg]) * p.group + hq - kvh * p.group;
+        const int* li = p.list_begin + seg * p.n_kv_heads + kvh;
+        b = li[0];
+        e = li[1];
+    }
+    int at = b + w0 + WPR * lane < e ? p.list[b + w0 + WPR * lane] + off : 0;
     pdl_wait();
-    if (r >= n_rows_out) return;
-    const int n_q_heads = p.n_kv_heads * p.group, t = r / n_q_heads, hq = r - t * n_q_heads, kvh = hq / p.group;
-    const int seg = p.seg_of_token[t];
-    const int off = (t - p.seg_first[seg]) * p.group + hq - kvh * p.group;
-    const int* li = p.list_begin + seg * p.n_kv_heads + kvh;
-    const int b = li[0], e = li[1];
     float m = -INFINITY, sum = 0.f, acc[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) acc[i] = 0.f;
-    for (int k0 = b; k0 < e; k0 += 32) {
-        const int n = min(32, e - k0);
-        int at = 0;
+    for (int k0 = b + w0; k0 < e; k0 += 32 * WPR) {
+        const int n = min(32, (e - k0 + WPR - 1) / WPR);
+        if (k0 != b + w0) at = lane < n ? p.list[k0 + WPR * lane] + off : 0;
         float2 ml = make_float2(-INFINITY, 0.f);
-        if (lane < n) {
-            at = p.list[k0 + lane] + off;
-            if ((unsigned)at < (unsigned)p.n_rows) ml = __ldcg(&p.part_ml[at]);
-            else {
-                atomicExch(p.status, 2);
-                at = 0;
-            }
+        if ((unsigned)at >= (unsigned)p.n_rows) {
+            atomicExch(p.status, 2);
+            at = 0;
         }
-        float mk = ml.y > 0.f || isnan(ml.y) ? ml.x : -INFINITY;   // a part in which the row sees nothing has no say
+        if (lane < n) ml = __ldcg(&p.part_ml[at]);
+        auto load = [&](int k, float (&v)[E]) {
+            const int ak = __shfl_sync(0xFFFFFFFFu, at, k & 31);
+            const float* src = p.part_o + (int64_t)ak * HD + lane * E;
+            if constexpr (E == 4) {
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(src));
+                v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+            } else {
+                const float2 x = __ldcg(reinterpret_cast<const float2*>(src));
+                v[0] = x.x; v[1] = x.y;
+            }
+        };
+        constexpr int U = WPR > 1 ? 8 : 4;
+        float v[U][E];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (u < n) load(u, v[u]);                         // on their way while the weights are made
+        const float mk = ml.y > 0.f || isnan(ml.y) ? ml.x : -INFINITY;   // a part in which the row sees nothing has no say
         float mn = mk;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, o));
@@ -582,23 +606,49 @@ shared_merge_kernel(SharedParams p, int n_rows_out) {
 #pragma unroll
         for (int i = 0; i < E; ++i) acc[i] *= corr;
         m = mn;
-#pragma unroll 4
-        for (int k = 0; k < n; ++k) {
-            const float wk = __shfl_sync(0xFFFFFFFFu, w, k);
-            const int ak = __shfl_sync(0xFFFFFFFFu, at, k);
-            const float* src = p.part_o + (int64_t)ak * HD + lane * E;
-            float v[E];
-            if constexpr (E == 4) {
-                const float4 x = __ldcg(reinterpret_cast<const float4*>(src));
-                v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-            } else {
-                const float2 x = __ldcg(reinterpret_cast<const float2*>(src));
-                v[0] = x.x; v[1] = x.y;
-            }
+        for (int k = 0;; ) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) acc[i] = wk > 0.f ? fmaf(v[i], wk, acc[i]) : acc[i];
+            for (int u = 0; u < U; ++u) {
+                if (k + u >= n) break;
+                const float wk = __shfl_sync(0xFFFFFFFFu, w, (k + u) & 31);
+#pragma unroll
+                for (int i = 0; i < E; ++i) acc[i] = wk > 0.f ? fmaf(v[u][i], wk, acc[i]) : acc[i];
+            }
+            k += U;
+            if (k >= n) break;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (k + u < n) load(k + u, v[u]);
         }
     }
+    if constexpr (WPR > 1) {
+        // the warps' results, joined the same way by the first
+#pragma unroll
+        for (int i = 0; i < E; ++i) part[warp][lane * E + i] = acc[i];
+        if (lane == 0) {
+            part[warp][HD] = m;
+            part[warp][HD + 1] = sum;
+        }
+        __syncthreads();
+        if (warp > 0) return;
+        float mn = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < WPR; ++k) mn = fmaxf(mn, part[k][HD]);
+        const float bs = mn == -INFINITY ? 0.f : mn;
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) acc[i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < WPR; ++k) {
+            const float w = ex2_approx(part[k][HD] - bs);
+            if (w > 0.f) {
+                sum = fmaf(w, part[k][HD + 1], sum);
+#pragma unroll
+                for (int i = 0; i < E; ++i) acc[i] = fmaf(w, part[k][lane * E + i], acc[i]);
+            }
+        }
+    }
+    if (r >= n_rows_out) return;
     const float inv = 1.f / sum;
     uint32_t o[E / 2];
 #pragma unroll

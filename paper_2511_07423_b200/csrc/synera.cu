@@ -495,7 +495,7 @@ static cudaError_t set_kernel_attributes() {
         kernel_smem(attn_kernel<128>, AttnSmem<128>::TOTAL), kernel_smem(attn_kernel<64>, AttnSmem<64>::TOTAL),
         kernel_smem(attn2_kernel<128>, Attn2Smem<128>::TOTAL), kernel_smem(attn2_kernel<64>, Attn2Smem<64>::TOTAL),
         kernel_smem(attn_shared_kernel<128>, SharedSmem<128>::TOTAL), kernel_smem(attn_shared_kernel<64>, SharedSmem<64>::TOTAL),
-        kernel_smem(shared_merge_kernel<128>, 0), kernel_smem(shared_merge_kernel<64>, 0),
+        kernel_smem(shared_merge_kernel<128, 1>, 0), kernel_smem(shared_merge_kernel<64, 1>, 0), kernel_smem(shared_merge_kernel<128, 4>, 0), kernel_smem(shared_merge_kernel<64, 4>, 0),
         kernel_smem(attn_thin_kernel<128>, AttnThinSmem<128>::TOTAL), kernel_smem(attn_thin_kernel<64>, AttnThinSmem<64>::TOTAL),
         kernel_smem(prep_kernel, 0), kernel_smem(verify_kernel, 0), kernel_smem(judging_rows_kernel, 0), kernel_smem(topk_rows_kernel, 0), kernel_smem(sample_verify_kernel, 0)};
     for (cudaError_t e : all)
@@ -1260,7 +1260,7 @@ static int attention_choice() { return g_attention == ATTN_SHARED ? 0 : g_attent
 
 // SM cycles of the shared-prefix kernel, fitted to the items' own times in the batches of the 8B and 32B shapes.
 static SharedCost shared_cost(const syn_model_desc& c) {
-    return c.head_dim == 128 ? SharedCost{3450, 11500, 2550, 4500, 1900, 3600, 14000} : SharedCost{2600, 9000, 2000, 4000, 1100, 5000, 14000};
+    return c.head_dim == 128 ? SharedCost{3450, 11500, 2550, 4500, 1900, 3600, 14000} : SharedCost{3350, 7500, 2080, 4000, 1700, 3600, 14000};
 }
 
 // Whether a batch planned as `hp` is better off with its common prefixes met once; fills `sp`.
@@ -1972,6 +1972,9 @@ static int launch_shared(syn_model* m, syn_kv* kv, const syn_plan* p, uint32_t l
         return SYN_E_CUDA;
     const bool wide = c.head_dim == 128;
     const int rows = p->T * (int)c.n_q_heads;
+    // a warp a row, or, where that leaves SMs without work, a block of four
+    const bool split = rows <= m->n_sm * SHR_MERGE_SPLIT_ROWS;
+    const dim3 grid_merge(split ? rows : (rows + 3) / 4);
     {
         ProfScope prof(m, 2, st);
         if ((wide ? launch_pdl(attn_shared_kernel<128>, dim3(p->n_cta), dim3(SHR_THREADS), SharedSmem<128>::TOTAL, st, tm, kv->tm_kv5, sp)
@@ -1979,8 +1982,8 @@ static int launch_shared(syn_model* m, syn_kv* kv, const syn_plan* p, uint32_t l
             return SYN_E_CUDA;
     }
     ProfScope prof(m, 3, st);
-    if ((wide ? launch_pdl(shared_merge_kernel<128>, dim3((rows + 3) / 4), dim3(128), 0, st, sp, rows)
-              : launch_pdl(shared_merge_kernel<64>, dim3((rows + 3) / 4), dim3(128), 0, st, sp, rows)) != cudaSuccess)
+    const auto merge = wide ? (split ? shared_merge_kernel<128, 4> : shared_merge_kernel<128, 1>) : (split ? shared_merge_kernel<64, 4> : shared_merge_kernel<64, 1>);
+    if (launch_pdl(merge, grid_merge, dim3(128), 0, st, sp, rows) != cudaSuccess)
         return SYN_E_CUDA;
     return SYN_OK;
 }
