@@ -356,25 +356,31 @@ class _Heads(C.Structure):
 
 def _heads(what: str, x: torch.Tensor, y: Optional[torch.Tensor], gain: Optional[torch.Tensor], tokens: int, hd: int, dtype, device: int) -> _Heads:
     """One operand [tokens, heads, hd] (heads side by side, any distance between tokens), checked; y: its output, in any shape
-    whose rows are a token's heads side by side."""
-    n, st = x.shape, x.stride()
-    if len(n) != 3 or n[0] != tokens or n[2] != hd or x.dtype != dtype or x.get_device() != device:
+    whose rows are a token's heads side by side.  (Written for few calls: a step makes this for every layer.)"""
+    st, y_at, y_stride, gain_at = x.stride(), None, 0, None
+    n = x.shape
+    if len(n) != 3 or n[0] != tokens or n[2] != hd or x.dtype is not dtype or x.get_device() != device:
         raise SynError(-1, f"{what}: {dtype} [{tokens}, heads, {hd}] on the current device")
-    heads, width = n[1], n[1] * hd
-    if (st[2] != 1 and hd > 1) or (st[1] != hd and heads > 1) or (st[0] < width and tokens > 1):
+    heads = n[1]
+    width = x_stride = heads * hd
+    if tokens > 1:
+        x_stride = st[0]
+    if st[2] != 1 or (st[1] != hd and heads > 1) or x_stride < width:
         raise SynError(-1, f"{what}: the heads of a token lie side by side")
-    ys = width
     if y is not None:
-        if y.get_device() != device or y.shape[0] != tokens or y.numel() != tokens * width:
+        if y.get_device() != device or y.numel() != tokens * width:
             raise SynError(-1, f"{what}: an output of {tokens} x {width} elements on the current device")
+        y_at, y_stride = y.data_ptr(), width
         if not y.is_contiguous():
-            if y.dim() != 3 or y.stride(2) != 1 or y.stride(1) != hd:
+            if y.dim() != 3 or y.shape[0] != tokens or y.stride(2) != 1 or y.stride(1) != hd:
                 raise SynError(-1, f"{what}: the heads of an output's token lie side by side")
-            ys = y.stride(0) if tokens > 1 else width
-    if gain is not None and (gain.dtype != torch.bfloat16 or gain.numel() != hd or not gain.is_contiguous() or gain.get_device() != device):
-        raise SynError(-1, f"{what}: gains are bfloat16 [{hd}] on the current device")
-    return _Heads(x.data_ptr(), y.data_ptr() if y is not None else None, gain.data_ptr() if gain is not None else None,
-                  st[0] if tokens > 1 else width, ys, heads)
+            if tokens > 1:
+                y_stride = y.stride(0)
+    if gain is not None:
+        if gain.dtype is not torch.bfloat16 or gain.shape != (hd,) or gain.stride() != (1,) or gain.get_device() != device:
+            raise SynError(-1, f"{what}: gains are bfloat16 [{hd}] on the current device")
+        gain_at = gain.data_ptr()
+    return _Heads(x.data_ptr(), y_at, gain_at, x_stride, y_stride, heads)
 
 
 def syn_op_qk_rope(rope: Optional[Rope], q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: Optional[torch.Tensor],
@@ -387,28 +393,35 @@ def syn_op_qk_rope(rope: Optional[Rope], q: Optional[torch.Tensor], k: Optional[
     if lead is None or lead.dim() != 3 or lead.dtype not in _TYPES:
         raise SynError(-1, "syn_op_qk_rope: q or k [T, heads, hd], bfloat16, float16 or float32")
     device = torch.cuda.current_device()
-    T, hd, dt = lead.shape[0], lead.shape[2], lead.dtype
-    if q is not None and q_out is None:
+    T, _, hd = lead.shape
+    dt = lead.dtype
+    if q is None:
+        q_out = None
+    elif q_out is None:
         q_out = torch.empty(q.shape, dtype=k_out.dtype if k is not None and k_out is not None else dt, device=q.device)
-    if k is not None and k_out is None:
+    if k is None:
+        k_out = None
+    elif k_out is None:
         k_out = torch.empty(k.shape, dtype=q_out.dtype if q is not None else dt, device=k.device)
-    odt = (q_out if q is not None else k_out).dtype
-    if odt not in _TYPES or (q is not None and k is not None and k_out.dtype != odt):
+    odt = (k_out if q is None else q_out).dtype
+    if odt not in _TYPES or (q is not None and k is not None and k_out.dtype is not odt):
         raise SynError(-1, "syn_op_qk_rope: both outputs have the inputs' dtype, or float16")
-    if rope is not None and (positions is None or positions.dtype != torch.int32 or positions.numel() != T or not positions.is_contiguous()
-                             or positions.get_device() != device):
-        raise SynError(-1, f"syn_op_qk_rope: positions are int32 [{T}] on the current device")
-    hq = _heads("q", q, q_out, q_gain, T, hd, dt, device) if q is not None else None
-    hk = _heads("k", k, k_out, k_gain, T, hd, dt, device) if k is not None else None
-    if T == 0:
-        return (q_out if q is not None else None), (k_out if k is not None else None)
-    code = load_library().syn_op_qk_rope(rope._h if rope is not None else None, C.addressof(hq) if hq is not None else None,
-                                         C.addressof(hk) if hk is not None else None,
-                                         positions.data_ptr() if rope is not None else None, T, hd, eps, _TYPES[dt], _TYPES[odt],
-                                         _raw_stream(stream, device))
-    if code:
-        _check(code, "syn_op_qk_rope")
-    return (q_out if q is not None else None), (k_out if k is not None else None)
+    rope_at = pos_at = hq = hk = None
+    if rope is not None:
+        if positions is None or positions.dtype is not torch.int32 or positions.shape != (T,) or not positions.is_contiguous() \
+                or positions.get_device() != device:
+            raise SynError(-1, f"syn_op_qk_rope: positions are int32 [{T}] on the current device")
+        rope_at, pos_at = rope._h, positions.data_ptr()
+    if q is not None:
+        hq = _heads("q", q, q_out, q_gain, T, hd, dt, device)
+    if k is not None:
+        hk = _heads("k", k, k_out, k_gain, T, hd, dt, device)
+    if T:
+        code = load_library().syn_op_qk_rope(rope_at, hq and C.addressof(hq), hk and C.addressof(hk), pos_at, T, hd, eps, _TYPES[dt], _TYPES[odt],
+                                             _raw_stream(stream, device))
+        if code:
+            _check(code, "syn_op_qk_rope")
+    return q_out, k_out
 
 
 class Plan:
