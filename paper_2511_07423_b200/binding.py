@@ -53,6 +53,8 @@ KERNEL_CLASSES = ("prep", "qkv_gemm", "attention", "attention_merge", "o_gemm", 
                   "lm_head_gemm", "verify", "judging_rows")
 
 
+SYN_MAX_CHUNK = 32
+
 _LIB: Optional[C.CDLL] = None
 
 EXPORTS = ["syn_model_load", "syn_model_free", "syn_kv_alloc", "syn_kv_free", "syn_kv_import", "syn_kv_export",

@@ -4,21 +4,29 @@
 // An item is some query tokens (of one request or of many), a kv head and a range of keys.  Its rows (row = j * G + g) are one
 // or two tiles of 128; every item leaves fp32 partials (m, l, O) per row, which shared_merge_kernel joins:
 //   out = sum_k 2^(m_k - m) O_k / sum_k 2^(m_k - m) l_k,  m = max_k m_k.
-// Both products run on tcgen05.mma with M = 128, in stages of 128 keys (8 pages):
-//   S = Q K^T : A = a Q tile, B = the stage's K, D = S in tensor memory (128 columns a tile);
-//   O += P V  : A = P in half precision in tensor memory, B = V as it lies in the cache, D = O.
+// Both products run on tcgen05.mma with M = 128, over half stages of 64 keys (a stage, 128 keys, is what the loads move):
+//   S = Q K^T : A = a Q tile, B = 64 keys of K, D = S in tensor memory (64 columns a group of warps);
+//   O += P V  : A = P in half precision in tensor memory (two buffers of 32 columns), B = V as it lies in the cache, D = O.
 // P in tensor memory leaves shared memory's bandwidth to the operands: with both of a product's operands there, a k-step of 64
-// cycles reads 8 KB, all that 128 bytes a cycle can deliver.
-// Two groups of four softmax warps (thread = row), each with its own S, P and O.  With two tiles a group owns a tile and takes
-// every stage: one read of K and V from L2 serves 256 rows, and while one group computes its exponentials the tensor
-// cores work for the other.  With one tile the groups take alternate stages, as in attention2.cuh, and leave separate partials.
-// What bounds it: with two tiles the exponentials (16 a cycle and SM, as many cycles as the products take at full rate) and the
-// products in turn; with one tile the keys' bytes.
+// cycles would read 8 KB, all that 128 bytes a cycle can deliver.
+// Two groups of four softmax warps (thread = row), each with its own S, P and O (SharedMode).  With two tiles a group owns a
+// tile: one read of K and V from L2 serves 256 rows.  With one tile the groups take alternate stages and leave separate partials,
+// or, where an item has few stages, one of them takes it while the other has the next item.
+//
 // Warp roles: warp 3 streams pages and Q tiles (K and V have rings of their own), one thread of warp 1 and one of warp 2 issue the
-// MMAs of a group each, warps 4..7 and 8..11 are the softmax groups.  tcgen05 operations of one thread complete in order, so Q K^T of a group's next stage may
-// follow P V of its last in the same columns, and the commit behind it tells that both are done.  The maximum that P is relative to
-// is raised only when a stage exceeds it by 2^8; P is scaled by 2^7 besides (at most 2^15 in half precision, so that weights down to
-// 2^-21 of the largest keep all their bits).  Every wait is bounded.
+// MMAs of a group each, warps 4..7 and 8..11 are the softmax groups.  tcgen05 operations of one thread complete in order, and a
+// commit tells that all before it are done.  The maximum that P is relative to is raised only when a half stage exceeds it by 2^8; P is
+// scaled by 2^7 besides (at most 2^15 in half precision, so that weights down to 2^-21 of the largest keep all their bits).
+// Every wait is bounded.
+//
+// What bounds it, on an 8B-shaped layer (32 query and 8 kv heads of 128): with two tiles a stage takes 3 430 cycles where the tensor
+// cores need 2 048 and the exponentials (16 a cycle) 2 048 too; a group's warps, one to a scheduler, wait for the latencies of
+// their own instructions, 860 cycles a half stage for the exponentials alone, which the two groups take in turns (shr_turn).  Above about
+// 900 TFLOP/s the power cap takes back what cycles are saved (1.6 GHz).  256 requests of 8 tokens on 12 016 shared keys: 409 us, 996 TFLOP/s
+// (24 chunks of 32 on 32 768 keys: 404 us, 1 035).  With one tile the keys' bytes: three requests on 131 072 keys 93 us, 5.8 TB/s.
+// Tried and slower (256 requests): P over S in shared columns with 128-key stages 490 us, one issuer for both groups 571; exponentials
+// not in turns 4 230 cycles a stage; a quarter of them by a polynomial on the multiply-add units 3 780; no maximum but a check of
+// the sum 4 800; the next half stage's scores fetched before this one's exponentials 750 us.
 #pragma once
 #include "attention2.cuh"
 #include "shared_plan.h"
@@ -83,8 +91,8 @@ __device__ __forceinline__ void umma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, ui
 }
 
 // The exponentials of the two groups' warps that share a scheduler, one warp after the other (a named barrier of each, which the
-// other arrives on when it is done): in step they would compete for the special-function unit and then leave it idle
-// together.  Both groups have as many turns (items of two tiles); the second group's first arrival lets the first begin.
+// other arrives on when it is done): in step they compete for the special-function unit and then leave it idle together.  Both
+// groups have as many turns (items of two tiles); the second group's first arrival lets the first begin.
 __device__ __forceinline__ void shr_turn(int wg, int wq) { asm volatile("bar.sync %0, 64;" ::"r"(1 + wg * 4 + wq) : "memory"); }
 __device__ __forceinline__ void shr_turn_over(int wg, int wq) { asm volatile("bar.arrive %0, 64;" ::"r"(1 + (wg ^ 1) * 4 + wq) : "memory"); }
 
@@ -217,9 +225,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         } else if ((warp == SHR_MMA_WARP0 || warp == SHR_MMA_WARP0 + 1) && elect_one()) {
             // -------------------------------------------------------- MMA issuers, one a group
             // A group works through half stages of 64 keys with one buffer of scores and two of P: as soon as its warps hold the
-            // scores of half u in registers, those of half u + 1 are computed, beside its exponentials; P V of half u follows.  (P
-            // over its own scores, in two buffers of these: the way P V, Q K^T, next scores was longer than a half stage's
-            // exponentials; 3 450 cycles a stage.  One issuer for both groups: 1 200 cycles a turn, 5 000 a stage.)
+            // scores of half u in registers, those of half u + 1 are computed, beside its exponentials; P V of half u follows.
             const int w = warp - SHR_MMA_WARP0;
             const uint32_t idesc_pv = umma_idesc_f16_bmn(128, HD), idesc_qk = umma_idesc_f16(128, SHR_HALF);
             const uint32_t o_tmem = tmem_base + w * 128, s_tmem = tmem_base + 256 + w * 128;

@@ -4,6 +4,8 @@
     python -m paper_2511_07423_b200.opbench attention --config 3
     python -m paper_2511_07423_b200.opbench sched --config 2 --rounds 8
     python -m paper_2511_07423_b200.opbench sample --config 3
+    python -m paper_2511_07423_b200.opbench prefix --config 3 --shared 4096
+    python -m paper_2511_07423_b200.opbench rope --config 3 --tokens 8192
     python -m paper_2511_07423_b200.opbench scale --config 2 --budgets 0.3,0.6,0.9 --rates 2,4,8,16,32
 
 `attention` builds a one-layer model with the attention geometry of the chosen configuration
@@ -14,6 +16,9 @@ chunks, prompts first), then each request offloads `--rounds` chunks drawn from 
 reports the iterations by kind and the share of the wall time spent in the scheduler's own code.
 `sample` times the sampling-verification stage (top-k of the logits rows + the per-request kernel)
 behind a one-layer model with the configuration's vocabulary and request mix.
+`prefix` times the attention of a batch whose requests share a prefix: the chosen configuration's heads and chunks, `--shared` common
+tokens and `--own` cached tokens of each request, with every request's keys read by itself and with the shared ones met once.
+`rope` times the per-head norm and rotation of queries and keys, and their append to the cache.
 `scale` is the scalability experiment of the paper's Sec. 6.4 in shape: the arrival-driven workload
 of workloads/arrivals.py (sessions arrive at a given rate, every device drafts chunks of gamma tokens
 at a fixed pace and offloads a chunk with probability = the offloading budget) with the scheduler over
@@ -94,6 +99,64 @@ def bench_attention(a):
                       "items": st.attn_items, "split_items": st.attn_split_items, "ms_attention": ms_att,
                       "ms_merge": ms_mrg, "kv_gbs": kvb / ms_att / 1e6, "kv_gbs_with_merge": kvb / (ms_att + ms_mrg) / 1e6,
                       "attn_tflops": st.attn_flops / ms_att / 1e9}))
+
+
+def _one_layer(name, s, seed):
+    return synthetic.load_model(ModelShape(f"{name}-{s.name}", 1, s.d_model, s.n_q_heads, s.n_kv_heads, s.head_dim, 1024, 1024), seed)
+
+
+def bench_prefix(a):
+    wl = CONFIGS[a.config]
+    s = wl.shape
+    model = _one_layer("prefix", s, wl.seed)
+    batch = gen.gen_batch(wl)
+    n, chunk = batch.n_req, batch.chunk_lens
+    common = a.shared // 16
+    ctx = torch.full((n,), common * 16 + a.own, dtype=torch.int32)
+    used = [-(-(int(ctx[i]) + int(chunk[i])) // 16) for i in range(n)]
+    table = torch.zeros(n, max(used), dtype=torch.int32)
+    at = common
+    for i, u in enumerate(used):
+        table[i, :common] = torch.arange(common, dtype=torch.int32)
+        table[i, common:u] = torch.arange(at, at + u - common, dtype=torch.int32)
+        at += u - common
+    kv = syn.KVCache(model, at)
+    kv.layer_view(0).normal_(0, 1)
+    T = batch.n_tokens
+    q = torch.empty(T, s.q_dim, dtype=torch.float16, device="cuda").normal_(0, 1.3)
+    out = torch.empty_like(q)
+    line = {"op": "prefix", "config": wl.name, "n_req": n, "T": T, "shared": common * 16, "own": a.own}
+    for name, share in (("each", False), ("shared", True)):
+        plan = syn.Plan(kv, torch.zeros(T, dtype=torch.int32), batch.chunk_offsets, table, ctx, share_prefix=share)
+        med, best = _time(lambda: plan.attention(0, q, out), a.iters)
+        st = plan.stats()
+        line.update({f"{name}_kernel": plan.attention_kernel(), f"{name}_ms": med, f"{name}_kv_bytes": st.kv_read_bytes, f"{name}_tflops": st.attn_flops / med / 1e9})
+    assert model.status() == 0
+    print(json.dumps(line))
+
+
+def bench_rope(a):
+    s = CONFIGS[a.config].shape
+    T, hq, hkv, hd = a.tokens, s.n_q_heads, s.n_kv_heads, s.head_dim
+    rope = syn.Rope(a.rotary or hd, s.rope_base, a.layout)
+    row = torch.empty(T, hq + 2 * hkv, hd, dtype=torch.bfloat16, device="cuda").normal_(0, 1)
+    q, k, v = row.split([hq, hkv, hkv], 1)
+    gq, gk = (torch.ones(hd, dtype=torch.bfloat16, device="cuda") if a.norm else None for _ in range(2))
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    oq, ok = torch.empty(T, hq, hd, dtype=torch.bfloat16, device="cuda"), torch.empty(T, hkv, hd, dtype=torch.bfloat16, device="cuda")
+    med, best = _time(lambda: syn.syn_op_qk_rope(rope, q, k, pos, gq, gk, s.rms_eps, oq, ok), a.iters)
+    by = 4 * T * (hq + hkv) * hd
+    model = _one_layer("rope", s, 0)
+    n = -(-T // syn.SYN_MAX_CHUNK)   # a batch of full chunks, each at the begin of a request
+    off = torch.tensor([min(T, i * syn.SYN_MAX_CHUNK) for i in range(n + 1)], dtype=torch.int32)
+    per = syn.SYN_MAX_CHUNK // 16
+    kv = syn.KVCache(model, per * n)
+    plan = syn.Plan(kv, torch.zeros(T, dtype=torch.int32), off, torch.arange(per * n, dtype=torch.int32).view(n, per), torch.zeros(n, dtype=torch.int32))
+    half = torch.empty(T, hq * hd, dtype=torch.float16, device="cuda")
+    app, _ = _time(lambda: plan.append(0, k, v, rope, gk, q, gq, half), a.iters)
+    by_app = 4 * T * (hq + 2 * hkv) * hd
+    print(json.dumps({"op": "rope", "tokens": T, "heads": [hq, hkv, hd], "layout": a.layout, "ms": med, "gbs": by / med / 1e6, "append_ms": app,
+                      "append_gbs": by_app / app / 1e6}))
 
 
 def bench_sched(a):
@@ -227,6 +290,18 @@ def main():
     t.add_argument("--pool-tokens", type=int, default=None)
     t.add_argument("--kind", type=int, default=0, help="attention kernel: 0 default, 1 warp-level MMAs, 2 tcgen05, 3 half-SM CTAs")
     t.add_argument("--iters", type=int, default=10)
+    f = sub.add_parser("prefix")
+    f.add_argument("--config", type=int, default=3)
+    f.add_argument("--shared", type=int, default=4096, help="tokens that all requests share (whole pages of 16)")
+    f.add_argument("--own", type=int, default=400, help="cached tokens of each request behind those")
+    f.add_argument("--iters", type=int, default=20)
+    o = sub.add_parser("rope")
+    o.add_argument("--config", type=int, default=3)
+    o.add_argument("--tokens", type=int, default=8192)
+    o.add_argument("--layout", default="half", choices=("half", "interleaved"))
+    o.add_argument("--rotary", type=int, default=0, help="components of a head that rotate (default: all)")
+    o.add_argument("--norm", action="store_true", help="per-head norms of queries and keys")
+    o.add_argument("--iters", type=int, default=20)
     m = sub.add_parser("sample")
     m.add_argument("--config", type=int, default=3)
     m.add_argument("--top-k", type=int, default=50)
@@ -249,7 +324,7 @@ def main():
     c.add_argument("--rounds", type=int, default=8)
     c.add_argument("--budget", type=int, default=2048, help="chunk tokens per iteration")
     a = ap.parse_args()
-    {"linear": bench_linear, "attention": bench_attention, "sched": bench_sched, "sample": bench_sample, "scale": bench_scale}[a.op](a)
+    {"linear": bench_linear, "attention": bench_attention, "sched": bench_sched, "sample": bench_sample, "prefix": bench_prefix, "rope": bench_rope, "scale": bench_scale}[a.op](a)
 
 
 if __name__ == "__main__":
