@@ -1291,7 +1291,17 @@ static int plan_build(syn_plan* p, syn_model* m, syn_kv* kv, int32_t n_req, cons
                          max_pages, ctx_lens, n_uncached, attention_choice(), thin_attention_ctas(m->n_sm), hp);
     if (r) return r;
     SharedPlan sp;
-    const bool shared = share && shared_better(m->desc, (int)kv->page_size, m->n_sm, n_req, chunk_offsets, page_tables, max_pages, ctx_lens, hp, sp);
+    bool shared = share && shared_better(m->desc, (int)kv->page_size, m->n_sm, n_req, chunk_offsets, page_tables, max_pages, ctx_lens, hp, sp);
+    if (shared) {   // without room for its partials the batch is planned as ever
+        if (cudaMalloc(&p->part_o, (size_t)sp.rows * m->desc.head_dim * 4) != cudaSuccess || cudaMalloc(&p->part_ml, (size_t)sp.rows * 8) != cudaSuccess) {
+            (void)cudaGetLastError();
+            cudaFree(p->part_o);
+            p->part_o = nullptr;
+            p->part_ml = nullptr;
+            shared = false;
+            sp = SharedPlan();
+        }
+    }
     if (shared) {
         hp.kind = ATTN_SHARED;
         hp.items.clear(); hp.groups.clear();
@@ -1351,8 +1361,6 @@ static int plan_build(syn_plan* p, syn_model* m, syn_kv* kv, int32_t n_req, cons
         memcpy(p->h<int>(p->o_list_begin), sp.list_begin.data(), sp.list_begin.size() * 4);
         memcpy(p->h<int>(p->o_list), sp.list.data(), sp.list.size() * 4);
         p->n_rows = (int)sp.rows; p->n_list = (int)sp.list.size(); p->n_seg = (int)sp.seg_first.size();
-        CU_OK(cudaMalloc(&p->part_o, (size_t)sp.rows * m->desc.head_dim * 4));
-        CU_OK(cudaMalloc(&p->part_ml, (size_t)sp.rows * 8));
     }
     p->n_req = n_req; p->T = T; p->max_pages = max_pages; p->n_items = n_items; p->n_cta = n_cta;
     p->n_groups = (int)hp.groups.size(); p->n_parts = hp.n_parts;
@@ -2686,7 +2694,7 @@ extern "C" int syn_op_qk_rope(const syn_rope* rope, const syn_heads* q, const sy
                               float eps, int32_t in_type, int32_t out_type, void* cuda_stream) {
     if ((!q && !k) || T < 0 || head_dim < 8 || head_dim > ROPE_MAX_DIM || head_dim % 8 || !(eps >= 0.f) || !rope_types_ok(in_type, out_type))
         return SYN_E_INVALID_ARG;
-    if (rope && (!positions || rope->rotary_dim > head_dim)) return SYN_E_INVALID_ARG;
+    if (rope && (!positions || ((uintptr_t)positions & 3) || rope->rotary_dim > head_dim)) return SYN_E_INVALID_ARG;
     RopeParams rp;
     memset(&rp, 0, sizeof(rp));
     if (rope) rp.rope = rope->table;

@@ -311,3 +311,26 @@ def test_the_step_over_shared_prefixes():
     clear = (two[:, 0] - two[:, 1]) > 0.12 * sigma
     assert torch.equal(ta[clear], tb[clear]) and bool(clear.any())
     assert float((pa.float() - pb.float()).abs().max()) <= 0.06 * float(pa.float().std())
+
+
+def test_without_room_for_partials_the_batch_is_planned_as_ever():
+    own, chunk, levels = [60] * 32, [32] * 32, [(300, 32)]                   # 60 MB of partials and more
+    model, kv, plan, pool, q, table, ctx, off = setup(own, chunk, levels, 128, 32, 8, force=False)
+    T = int(off[-1])
+    assert plan.attention_kernel() == 4
+    want = plan.attention(1, q)
+    plain = syn.Plan(kv, torch.zeros(T, dtype=torch.int32), off, table, ctx)   # (the model's workspaces are there)
+    plan.close()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    fill = torch.empty(torch.cuda.mem_get_info()[0] - (16 << 20), dtype=torch.uint8, device="cuda")
+    assert torch.cuda.mem_get_info()[0] < 24 << 20                           # the plan's lists fit, its partials do not
+    again = syn.Plan(kv, torch.zeros(T, dtype=torch.int32), off, table, ctx, share_prefix=True)
+    assert again.attention_kernel() == plain.attention_kernel() != 4
+    del fill
+    torch.cuda.empty_cache()
+    got = again.attention(1, q)
+    size = pool.abs().max().double()
+    # two results of the same formula, each within 2^-11 of the weights and of the value
+    assert float((got.double() - want.double()).abs().max()) <= float(2 * (2 * 2.0 ** -11 + 2.0 ** -14) * size)
+    assert model.status() == 0

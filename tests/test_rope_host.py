@@ -98,6 +98,7 @@ def test_the_c_entry_checks_shapes_before_it_touches_the_device():
     assert call(xs=255) == -1 and call(ys=255) == -1
     assert call(x=None) == -1 and call(y=None) == -1 and call(pos=None) == -1
     assert call(x=(1 << 20) + 1) == -1 and call(y=(1 << 30) + 1) == -1 and call(gain=(1 << 12) + 1) == -1
+    assert call(pos=(1 << 12) + 2) == -1
     assert call(it=3) == -1 and call(it=-1) == -1 and call(it=1, ot=0) == -1 and call(it=0, ot=2) == -1
     assert call(eps=-1.0) == -1 and call(eps=math.nan) == -1
     assert call(y=1 << 20, ys=512) == -1                       # in place with another stride

@@ -48,6 +48,7 @@ CASES = [   # own cached tokens, chunks, levels of (pages, group), (hd, hq, hkv)
     ([10, 20], [4, 4], [(7, 2)], (128, 8, 1), 148),                    # too little in common for a node
     ([2000], [17], [(0, 1)], (64, 32, 8), 148),
     ([5] * 33, [1, 2, 3] * 11, [(100, 33), (40, 11)], (128, 7, 1), 5),
+    ([70, 3, 0, 9], [2, 30, 1, 7], [(25, 4), (9, 2)], (64, 6, 2), 1),     # one CTA has it all
     ([9] * 64, [1] * 64, [(90, 64)], (128, 8, 8), 148),                # one query head to a kv head
 ]
 
