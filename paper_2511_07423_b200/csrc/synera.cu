@@ -1260,16 +1260,20 @@ static int attention_choice() { return g_attention == ATTN_SHARED ? 0 : g_attent
 
 // SM cycles of the shared-prefix kernel, fitted to the items' own times in the batches of the 8B and 32B shapes.
 static SharedCost shared_cost(const syn_model_desc& c) {
-    return c.head_dim == 128 ? SharedCost{3450, 11500, 2550, 4500, 1900, 3600, 14000} : SharedCost{3350, 7500, 2080, 4000, 1700, 3600, 14000};
+    return c.head_dim == 128 ? SharedCost{3450, 11500, 2550, 4500, 1900, 3600, 14000} : SharedCost{3350, 7500, 2080, 4000, 1700, 3600, 11500};
 }
 
-// Whether a batch planned as `hp` is better off with its common prefixes met once; fills `sp`.
+// Whether a batch planned as `hp` is better off on the shared-prefix kernel; fills `sp`.  Where nothing is shared that kernel still cuts
+// the keys of a few long requests into more and shorter items (2 requests of 29 589 keys, 16 tokens, 14 heads on 2 of 128: 23 us against 125;
+// one of 20 064, 4 tokens: 13 against 25), and has to be estimated 15 % better there, for the batch is otherwise the plan without
+// sharing, whose results do not depend on this.  Against the better kernel of each batch the choice loses 2.6 % in 48 batches that
+// share nothing (23 % when it kept to the other kernels there; 0.9 % with 8 % for 15), 1.1 % in 120 that do or are one request.
 static bool shared_better(const syn_model_desc& c, int P, int n_sm, int32_t n_req, const int32_t* chunk_offsets, const int32_t* page_tables,
                           int32_t max_pages, const int32_t* ctx_lens, const HostPlan& hp, SharedPlan& sp) {
     if (g_attention != 0 && g_attention != ATTN_SHARED) return false;
     shared_plan(n_req, chunk_offsets, page_tables, max_pages, ctx_lens, P, c.n_q_heads / c.n_kv_heads, c.n_kv_heads, n_sm, shared_cost(c), sp);
     if (sp.rows > (int64_t)1 << 30) return false;
-    return g_attention == ATTN_SHARED || (sp.shares && sp.estimate < hp.estimate);
+    return g_attention == ATTN_SHARED || sp.estimate * 100 < hp.estimate * (sp.shares ? 100 : 85);
 }
 
 // The step's counters of a batch whose attention runs over shared prefixes: every shared key is read once.

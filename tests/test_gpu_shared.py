@@ -99,6 +99,17 @@ def test_matches_the_formula(own, chunk, levels, heads):
     assert model.status() == 0
 
 
+@pytest.mark.parametrize("own,chunk,heads", [([4149], [8], (128, 14, 2)), ([10460], [8], (128, 8, 1)), ([7818], [8], (64, 4, 2)),
+                                             ([29589, 12000], [16, 5], (128, 14, 2))])
+def test_a_few_long_requests_are_cut_finer(own, chunk, heads):
+    """Nothing is shared, and the planner takes the kernel of shared prefixes by itself."""
+    model, kv, plan, pool, q, table, ctx, off = setup(own, chunk, [], *heads, force=False)
+    assert plan.attention_kernel() == 4
+    want, size = reference(pool, q, table, ctx, off)
+    check(plan.attention(1, q), want, size)
+    assert model.status() == 0
+
+
 def test_values_behind_a_request_do_not_reach_it():
     """Whatever lies behind the last token of a request, in its own last page and in pages it never reaches: infinities and no
     numbers, in K and in V.  Chunks end at every place of a page."""

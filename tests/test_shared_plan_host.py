@@ -136,6 +136,15 @@ def test_nothing_shared_is_planned_as_ever():
     assert syn.plan_shared_host(shape(128, 32, 8), n_pages, torch.zeros(80, dtype=torch.int32), off, table, ctx)["taken"]
 
 
+def test_a_few_long_requests_are_cut_finer():
+    for own, heads in (([4149], (128, 14, 2)), ([10460], (128, 8, 1)), ([29589, 12000], (128, 14, 2))):
+        table, ctx, off, n_pages = tree_batch(random.Random(5), own, [8] * len(own), [])
+        p = syn.plan_shared_host(shape(*heads), n_pages, torch.zeros(8 * len(own), dtype=torch.int32), off, table, ctx)
+        assert p["taken"] and not any(r[6] < 0 for r in p["items"].tolist())
+        plain = syn.plan_host(shape(*heads), n_pages, torch.zeros(8 * len(own), dtype=torch.int32), off, table, ctx)["stats"]
+        assert p["stats"].kv_read_bytes == plain.kv_read_bytes
+
+
 def test_many_requests_in_a_chain_of_prefixes():
     # request i shares i * 8 pages with request i + 1: a path of nested runs
     n, rows = 60, []
