@@ -53,7 +53,7 @@ struct SharedParams {
     int* status;                 // 0 ok, 1 a bounded wait ran out, 2 the work list failed a bounds check
     const int *seg_of_token, *seg_first, *list_begin, *list;   // SharedPlan's
     op16* out;                   // [T][q_dim]
-    int n_items, n_req, n_tokens, n_pages, n_rows, n_list, n_seg;
+    int n_items, n_req, n_tokens, n_pages, n_rows;
 };
 
 // The work list is host-made; the kernel still refuses an item that would index out of bounds.

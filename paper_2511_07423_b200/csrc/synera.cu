@@ -376,7 +376,7 @@ struct syn_plan {
     int n_judging = 0;       // rows whose argmax verification looks at: a request's from its last uncached token on
     // attention over shared prefixes (ATTN_SHARED): the work list's and the merge's arrays, and the plan's own partials
     size_t o_seg, o_seg_first, o_list_begin, o_list;
-    int n_rows = 0, n_list = 0, n_seg = 0;
+    int n_rows = 0;
     float* part_o = nullptr;
     float2* part_ml = nullptr;
     // the cache the page ids and slots were validated against
@@ -1364,7 +1364,7 @@ static int plan_build(syn_plan* p, syn_model* m, syn_kv* kv, int32_t n_req, cons
         memcpy(p->h<int>(p->o_seg_first), sp.seg_first.data(), sp.seg_first.size() * 4);
         memcpy(p->h<int>(p->o_list_begin), sp.list_begin.data(), sp.list_begin.size() * 4);
         memcpy(p->h<int>(p->o_list), sp.list.data(), sp.list.size() * 4);
-        p->n_rows = (int)sp.rows; p->n_list = (int)sp.list.size(); p->n_seg = (int)sp.seg_first.size();
+        p->n_rows = (int)sp.rows;
     }
     p->n_req = n_req; p->T = T; p->max_pages = max_pages; p->n_items = n_items; p->n_cta = n_cta;
     p->n_groups = (int)hp.groups.size(); p->n_parts = hp.n_parts;
@@ -1973,7 +1973,7 @@ static int launch_shared(syn_model* m, syn_kv* kv, const syn_plan* p, uint32_t l
     sp.list_begin = p->d<int>(p->o_list_begin); sp.list = p->d<int>(p->o_list);
     sp.out = out;
     sp.n_items = p->n_items; sp.n_req = p->n_req; sp.n_tokens = p->T; sp.n_pages = (int)kv->n_pages;
-    sp.n_rows = p->n_rows; sp.n_list = p->n_list; sp.n_seg = p->n_seg;
+    sp.n_rows = p->n_rows;
     // a tile: one 64-dim half of the G heads of a kv head for 128 / G tokens, i.e. rows (token, head) of 128 bytes
     CUtensorMap tm;
     cuuint64_t dims[4] = {64, c.head_dim / 64, c.n_q_heads, (cuuint64_t)p->T};
