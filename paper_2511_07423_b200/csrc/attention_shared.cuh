@@ -598,14 +598,18 @@ shared_merge_kernel(SharedParams p, int n_rows_out) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u < n) load(u, v[u]);                         // on their way while the weights are made
-        const float mk = ml.y > 0.f || isnan(ml.y) ? ml.x : -INFINITY;   // a part in which the row sees nothing has no say
+        // A part in which the row sees nothing (its sum is zero) has no say.  Every other counts even where its weight is zero: a sum or
+        // a result that is no number (maybe its reference exponent too) stays none.
+        const bool say = ml.y != 0.f;
+        const uint32_t says = __ballot_sync(0xFFFFFFFFu, say);
+        const float mk = say ? ml.x : -INFINITY;
         float mn = mk;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, o));
         mn = fmaxf(m, mn);
         const float bs = mn == -INFINITY ? 0.f : mn, corr = ex2_approx(m - bs);
         const float w = ex2_approx(mk - bs);
-        float ws = w > 0.f ? w * ml.y : 0.f;
+        float ws = w * ml.y;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) ws += __shfl_xor_sync(0xFFFFFFFFu, ws, o);
         sum = sum * corr + ws;
@@ -618,7 +622,7 @@ shared_merge_kernel(SharedParams p, int n_rows_out) {
                 if (k + u >= n) break;
                 const float wk = __shfl_sync(0xFFFFFFFFu, w, (k + u) & 31);
 #pragma unroll
-                for (int i = 0; i < E; ++i) acc[i] = wk > 0.f ? fmaf(v[u][i], wk, acc[i]) : acc[i];
+                for (int i = 0; i < E; ++i) acc[i] = says >> ((k + u) & 31) & 1u ? fmaf(v[u][i], wk, acc[i]) : acc[i];
             }
             k += U;
             if (k >= n) break;
@@ -647,7 +651,7 @@ shared_merge_kernel(SharedParams p, int n_rows_out) {
 #pragma unroll
         for (int k = 0; k < WPR; ++k) {
             const float w = ex2_approx(part[k][HD] - bs);
-            if (w > 0.f) {
+            if (part[k][HD + 1] != 0.f) {   // (as above)
                 sum = fmaf(w, part[k][HD + 1], sum);
 #pragma unroll
                 for (int i = 0; i < E; ++i) acc[i] = fmaf(w, part[k][lane * E + i], acc[i]);
