@@ -406,6 +406,7 @@ attn2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             const float bs_all = m_all == -INFINITY ? 0.f : m_all;
             const float wa = ex2_approx(m_used - bs_all), wb = ex2_approx(other.x - bs_all);   // -inf -> 0
             const float l_all = l * wa + other.y * wb;
+            const bool has_a = l != 0.f, has_b = other.y != 0.f;   // the row sees keys of the group's (a sum that is no number counts)
             if (ok) ok = wait_all(o_full, (uint32_t)qi & 1u);
             if (ok) {
                 tc_fence_after();
@@ -419,8 +420,8 @@ attn2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                     tmem_ld_wait();
                     float v[32];
 #pragma unroll
-                    for (int c = 0; c < 32; ++c)   // a group without a stage in this item holds stale numbers: weight 0 drops them
-                        v[c] = (wa > 0.f ? __uint_as_float(oa[c]) * fa : 0.f) + (wb > 0.f ? __uint_as_float(ob[c]) * fb : 0.f);
+                    for (int c = 0; c < 32; ++c)   // a group without a stage in this item holds stale numbers, and is left out
+                        v[c] = (has_a ? __uint_as_float(oa[c]) * fa : 0.f) + (has_b ? __uint_as_float(ob[c]) * fb : 0.f);
                     if (live) {
                         if (item.part < 0) {
                             uint4* dst = reinterpret_cast<uint4*>(p.out + (size_t)(item.q_tok + j) * p.q_dim + (item.kvh * G + gq) * HD + ch * 32);
