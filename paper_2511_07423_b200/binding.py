@@ -321,7 +321,8 @@ class _RopeDesc(C.Structure):
 
 class Rope:
     """syn_rope_create / syn_rope_freqs / syn_rope_free: a rotation of the leading `rotary_dim` components of a head, in
-    halves or interleaved, with its frequencies as they are or scaled ("linear", "base", "turns", "index")."""
+    halves or interleaved, with its frequencies as they are or scaled ("linear", "base", "turns", "index").  Calls that are
+    given it after close() are refused."""
 
     def __init__(self, rotary_dim: int, base: float = 10000.0, layout: str = "half", scaling: str = "none", factor: float = 1.0,
                  original_len: float = 0.0, low: float = 0.0, high: float = 0.0, amplitude: float = 0.0):
@@ -349,6 +350,15 @@ class Rope:
             self.close()
         except Exception:
             pass
+
+
+def _rope_handle(rope: Optional[Rope]) -> Optional[C.c_void_p]:
+    # to the library a null handle is "no rotation", which a closed rotation is not
+    if rope is None:
+        return None
+    if not rope._h:
+        raise SynError(-1, "the rotation was closed")
+    return rope._h
 
 
 class _Heads(C.Structure):
@@ -391,6 +401,7 @@ def syn_op_qk_rope(rope: Optional[Rope], q: Optional[torch.Tensor], k: Optional[
     """syn_op_qk_rope: per-head norm (where a gain is given) and rotation of q [T, heads, hd] and k [T, kv heads, hd], either of
     which may be None; slices of one projection's rows are fine.  positions: int32 [T].  The outputs have the inputs' dtype unless
     q_out / k_out (both, of one dtype) say float16; they may be the inputs themselves.  Returns (q_out, k_out)."""
+    rope_at = _rope_handle(rope)
     lead = q if q is not None else k
     if lead is None or lead.dim() != 3 or lead.dtype not in _TYPES:
         raise SynError(-1, "syn_op_qk_rope: q or k [T, heads, hd], bfloat16, float16 or float32")
@@ -408,12 +419,12 @@ def syn_op_qk_rope(rope: Optional[Rope], q: Optional[torch.Tensor], k: Optional[
     odt = (k_out if q is None else q_out).dtype
     if odt not in _TYPES or (q is not None and k is not None and k_out.dtype is not odt):
         raise SynError(-1, "syn_op_qk_rope: both outputs have the inputs' dtype, or float16")
-    rope_at = pos_at = hq = hk = None
+    pos_at = hq = hk = None
     if rope is not None:
         if positions is None or positions.dtype is not torch.int32 or positions.shape != (T,) or not positions.is_contiguous() \
                 or positions.get_device() != device:
             raise SynError(-1, f"syn_op_qk_rope: positions are int32 [{T}] on the current device")
-        rope_at, pos_at = rope._h, positions.data_ptr()
+        pos_at = positions.data_ptr()
     if q is not None:
         hq = _heads("q", q, q_out, q_gain, T, hd, dt, device)
     if k is not None:
@@ -462,6 +473,7 @@ class Plan:
         """syn_op_kv_append: normalises (k_gain) and rotates (rope) the chunks' keys k [T, n_kv_heads, hd] and puts them, with
         v, into the layer at the plan's slots.  With q [T, n_q_heads, hd]: returns the queries, treated the same way, as attention()
         takes them, float16 [T, n_q_heads * hd]."""
+        rope_at = _rope_handle(rope)
         s = self.kv.model.shape
         device, T, hd = torch.cuda.current_device(), self.n_tokens, s.head_dim
         dt = k.dtype
@@ -473,7 +485,7 @@ class Plan:
             raise SynError(-1, "append: the queries' output is float16")
         hq = _heads("q", q, q_out, q_gain, T, hd, dt, device) if q is not None else None
         hk, hv = _heads("k", k, None, k_gain, T, hd, dt, device), _heads("v", v, None, None, T, hd, dt, device)
-        code = self._lib.syn_op_kv_append(self.kv.model._h, self.kv._h, self._h, layer, rope._h if rope is not None else None,
+        code = self._lib.syn_op_kv_append(self.kv.model._h, self.kv._h, self._h, layer, rope_at,
                                           C.addressof(hq) if hq is not None else None, C.addressof(hk), C.addressof(hv), _TYPES[dt],
                                           _raw_stream(stream, device))
         if code:
