@@ -367,8 +367,8 @@ class _Heads(C.Structure):
 
 
 def _heads(what: str, x: torch.Tensor, y: Optional[torch.Tensor], gain: Optional[torch.Tensor], tokens: int, hd: int, dtype, device: int) -> _Heads:
-    """One operand [tokens, heads, hd] (heads side by side, any distance between tokens), checked; y: its output, in any shape
-    whose rows are a token's heads side by side.  (Written for few calls: a step makes this for every layer.)"""
+    """One operand [tokens, heads, hd] (heads side by side, any distance between tokens), checked; y: its output, contiguous in any shape
+    (token by token, a token's heads side by side), or [tokens, heads, hd] with any distance between tokens.  (Written for few calls: a step makes this for every layer.)"""
     st, y_at, y_stride, gain_at = x.stride(), None, 0, None
     n = x.shape
     if len(n) != 3 or n[0] != tokens or n[2] != hd or x.dtype is not dtype or x.get_device() != device:
@@ -384,7 +384,7 @@ def _heads(what: str, x: torch.Tensor, y: Optional[torch.Tensor], gain: Optional
             raise SynError(-1, f"{what}: an output of {tokens} x {width} elements on the current device")
         y_at, y_stride = y.data_ptr(), width
         if not y.is_contiguous():
-            if y.dim() != 3 or y.shape[0] != tokens or y.stride(2) != 1 or y.stride(1) != hd:
+            if y.shape != (tokens, heads, hd) or y.stride(2) != 1 or (y.stride(1) != hd and heads > 1):
                 raise SynError(-1, f"{what}: the heads of an output's token lie side by side")
             if tokens > 1:
                 y_stride = y.stride(0)
@@ -400,7 +400,8 @@ def syn_op_qk_rope(rope: Optional[Rope], q: Optional[torch.Tensor], k: Optional[
                    q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
     """syn_op_qk_rope: per-head norm (where a gain is given) and rotation of q [T, heads, hd] and k [T, kv heads, hd], either of
     which may be None; slices of one projection's rows are fine.  positions: int32 [T].  The outputs have the inputs' dtype unless
-    q_out / k_out (both, of one dtype) say float16; they may be the inputs themselves.  Returns (q_out, k_out)."""
+    q_out / k_out (both, of one dtype) say float16; they may be the inputs themselves, slices of rows like them, or contiguous in another
+    shape, whose memory is then filled token by token.  Returns (q_out, k_out)."""
     rope_at = _rope_handle(rope)
     lead = q if q is not None else k
     if lead is None or lead.dim() != 3 or lead.dtype not in _TYPES:
