@@ -119,6 +119,17 @@ def _raw_stream(stream: Optional[torch.cuda.Stream], device: int) -> int:
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
+def _empty(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """Memory for the result of a call on `stream`: that stream's own, for what the current stream has let go may still be in use
+    there; and what the current stream does with the result counts when it is let go."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        y = torch.empty(shape, dtype=dtype, device=device)
+    y.record_stream(torch.cuda.current_stream(y.device))
+    return y
+
+
 class Model:
     """syn_model_load / syn_model_free."""
 
@@ -211,8 +222,7 @@ class KVCache:
     def export_kv(self, layer: int, page_table, pos0: int, n_pos: int, stream=None):
         s = self.model.shape
         pt = _i32(page_table)
-        k = torch.empty(n_pos, s.n_kv_heads, s.head_dim, dtype=torch.bfloat16, device="cuda")
-        v = torch.empty_like(k)
+        k, v = (_empty((n_pos, s.n_kv_heads, s.head_dim), torch.bfloat16, "cuda", stream) for _ in range(2))
         _check(self._lib.syn_kv_export(self._h, C.c_uint32(layer), C.c_void_p(pt.data_ptr()), C.c_int32(pos0),
                                        C.c_int32(n_pos), C.c_void_p(k.data_ptr()), C.c_void_p(v.data_ptr()),
                                        _stream_ptr(stream)), "syn_kv_export")
@@ -252,7 +262,7 @@ class KVCache:
         assert acc.dtype == torch.int32 and cor.dtype == torch.int32 and not acc.is_cuda and acc.numel() >= n_req
         logits = None
         if want_logits:
-            logits = torch.empty(int(off[-1]), self.model.shape.vocab, dtype=torch.float32, device="cuda")
+            logits = _empty((int(off[-1]), self.model.shape.vocab), torch.float32, "cuda", stream)
         ids = torch.as_tensor(req_ids, dtype=torch.int64).contiguous() if req_ids is not None else None
         _check(self._lib.syn_verify_batch(
             self.model._h, self._h, C.c_int32(n_req), C.c_void_p(ids.data_ptr()) if ids is not None else None,
@@ -281,7 +291,7 @@ def verify_batch_sampled(kv: "KVCache", chunk_tokens, chunk_offsets, page_tables
     sid, sp, ra, rs = _i32(slm_ids), _f32(slm_probs), _f32(rand_accept), _f32(rand_sample)
     acc = torch.empty(n_req, dtype=torch.int32)
     cor = torch.empty(n_req, dtype=torch.int32)
-    logits = torch.empty(int(off[-1]), kv.model.shape.vocab, dtype=torch.float32, device="cuda") if want_logits else None
+    logits = _empty((int(off[-1]), kv.model.shape.vocab), torch.float32, "cuda", stream) if want_logits else None
     _check(load_library().syn_verify_batch_sampled(
         kv.model._h, kv._h, C.c_int32(n_req), None, C.c_void_p(tok.data_ptr()), C.c_void_p(off.data_ptr()),
         C.c_void_p(pt.data_ptr()), C.c_int32(pt.shape[1]), C.c_void_p(ctx.data_ptr()),
@@ -412,11 +422,11 @@ def syn_op_qk_rope(rope: Optional[Rope], q: Optional[torch.Tensor], k: Optional[
     if q is None:
         q_out = None
     elif q_out is None:
-        q_out = torch.empty(q.shape, dtype=k_out.dtype if k is not None and k_out is not None else dt, device=q.device)
+        q_out = _empty(q.shape, k_out.dtype if k is not None and k_out is not None else dt, q.device, stream)
     if k is None:
         k_out = None
     elif k_out is None:
-        k_out = torch.empty(k.shape, dtype=q_out.dtype if q is not None else dt, device=k.device)
+        k_out = _empty(k.shape, q_out.dtype if q is not None else dt, k.device, stream)
     odt = (k_out if q is None else q_out).dtype
     if odt not in _TYPES or (q is not None and k is not None and k_out.dtype is not odt):
         raise SynError(-1, "syn_op_qk_rope: both outputs have the inputs' dtype, or float16")
@@ -481,7 +491,7 @@ class Plan:
         if dt not in _TYPES:
             raise SynError(-1, "append: bfloat16, float16 or float32")
         if q is not None and q_out is None:
-            q_out = torch.empty(T, s.q_dim, dtype=torch.float16, device=q.device)
+            q_out = _empty((T, s.q_dim), torch.float16, q.device, stream)
         if q is not None and q_out.dtype != torch.float16:
             raise SynError(-1, "append: the queries' output is float16")
         hq = _heads("q", q, q_out, q_gain, T, hd, dt, device) if q is not None else None
@@ -497,7 +507,7 @@ class Plan:
         """syn_op_attention: q and the result are half precision [T, n_q_heads * head_dim]."""
         assert q.is_cuda and q.dtype == torch.float16 and q.is_contiguous()
         if out is None:
-            out = torch.empty_like(q)
+            out = _empty(q.shape, q.dtype, q.device, stream)
         _check(self._lib.syn_op_attention(self.kv.model._h, self.kv._h, self._h, C.c_uint32(layer),
                                           C.c_void_p(q.data_ptr()), C.c_void_p(out.data_ptr()), _stream_ptr(stream)),
                "syn_op_attention")
@@ -516,7 +526,7 @@ class Plan:
         the call itself free of allocations on the Python side too."""
         assert q.is_cuda and q.dtype == torch.float16 and q.is_contiguous()
         if out is None:
-            out = torch.empty_like(q)
+            out = _empty(q.shape, q.dtype, q.device, stream)
         _check(self._lib.syn_op_attention_static(self.kv.model._h, self.kv._h, self._h, C.c_uint32(layer),
                                                  C.c_void_p(q.data_ptr()), C.c_void_p(out.data_ptr()),
                                                  _stream_ptr(stream)), "syn_op_attention_static")
@@ -811,7 +821,7 @@ def syn_op_linear(x: torch.Tensor, w: torch.Tensor, stream=None, schedule_as: st
     x, w = x.contiguous(), w.contiguous()
     T, K = x.shape
     N = w.shape[0]
-    y = torch.empty(T, N, dtype=torch.float32, device="cuda")
+    y = _empty((T, N), torch.float32, "cuda", stream)
     lib = load_library()
     if not reuse_pack:
         _check(lib.syn_op_linear_reset(), "syn_op_linear_reset")
