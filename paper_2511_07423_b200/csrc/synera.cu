@@ -1303,9 +1303,9 @@ static int plan_build(syn_plan* p, syn_model* m, syn_kv* kv, int32_t n_req, cons
             p->part_o = nullptr;
             p->part_ml = nullptr;
             shared = false;
-            sp = SharedPlan();
         }
     }
+    if (!shared) sp = SharedPlan();   // a work list that is not taken leaves nothing in the plan
     if (shared) {
         hp.kind = ATTN_SHARED;
         hp.items.clear(); hp.groups.clear();
