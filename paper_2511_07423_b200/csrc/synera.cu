@@ -1296,15 +1296,6 @@ static int plan_build(syn_plan* p, syn_model* m, syn_kv* kv, int32_t n_req, cons
     if (r) return r;
     SharedPlan sp;
     bool shared = share && shared_better(m->desc, (int)kv->page_size, m->n_sm, n_req, chunk_offsets, page_tables, max_pages, ctx_lens, hp, sp);
-    if (shared) {   // without room for its partials the batch is planned as ever
-        if (cudaMalloc(&p->part_o, (size_t)sp.rows * m->desc.head_dim * 4) != cudaSuccess || cudaMalloc(&p->part_ml, (size_t)sp.rows * 8) != cudaSuccess) {
-            (void)cudaGetLastError();
-            cudaFree(p->part_o);
-            p->part_o = nullptr;
-            p->part_ml = nullptr;
-            shared = false;
-        }
-    }
     if (!shared) sp = SharedPlan();   // a work list that is not taken leaves nothing in the plan
     if (shared) {
         hp.kind = ATTN_SHARED;
@@ -1342,6 +1333,10 @@ static int plan_build(syn_plan* p, syn_model* m, syn_kv* kv, int32_t n_req, cons
         CU_OK(cudaMalloc(&p->dev, cap));
         CU_OK(cudaMallocHost(&p->host, cap));
         p->cap = cap;
+    }
+    if (shared) {
+        CU_OK(cudaMalloc(&p->part_o, (size_t)sp.rows * m->desc.head_dim * 4));
+        CU_OK(cudaMalloc(&p->part_ml, (size_t)sp.rows * 8));
     }
     p->used = off;
     memcpy(p->h<int>(p->o_tokens), chunk_tokens, (size_t)T * 4);
@@ -1448,6 +1443,9 @@ static int syn_plan_create_impl(syn_model* m, syn_kv* kv, int32_t n_req, const i
     if (r == SYN_OK) r = ensure_workspace(m, p->T, p->n_parts);
     if (r != SYN_OK) {
         syn_plan_free(p);
+        // without room for a shared plan's lists, its partials and the step's workspaces together the batch is planned as ever
+        if (r == SYN_E_OOM && share)
+            return syn_plan_create_impl(m, kv, n_req, chunk_tokens, chunk_offsets, page_tables, max_pages, ctx_lens, n_uncached, false, out);
         return r;
     }
     *out = p;
