@@ -179,7 +179,9 @@ void syn_plan_free(syn_plan *p);
  * the page tables: requests next to each other in the batch whose rows begin with the same pages share those that are full
  * and cached for each of them (page i where (i + 1) * page_size <= ctx_lens), from 128 keys on; runs of neighbours that have more
  * in common than the run around them form further levels.  So put requests that share next to each other.  The
- * batch is planned as by syn_plan_create where the planner expects no gain or the device has no room for the partial results;
+ * batch is planned as by syn_plan_create where the planner expects no gain or the device has no room for the partial results, which are
+ * at most 4 head_dim + 8 bytes times the larger of 2^19 and 8 rows a token and query head (where more levels would leave
+ * more, a level has to be 256 keys to count, and so on);
  * syn_plan_attention tells (4: shared, also where nothing is shared but a few long requests are better cut that way).  A shared
  * plan holds the fp32 partial results of its own attention (calls on one plan must not overlap), so
  * syn_op_attention and syn_op_attention_static allocate nothing and copy nothing with it: q there is read in place and must be

@@ -102,9 +102,14 @@ inline std::vector<SharedNode> shared_tree(int n_req, const int* page_tables, in
     return nodes;
 }
 
-inline void shared_plan(int n_req, const int* chunk_offsets, const int* page_tables, int max_pages, const int* ctx_lens, int page_size,
-                        int group, int n_kv_heads, int n_sm, const SharedCost& cost, SharedPlan& sp) {
-    const std::vector<SharedNode> nodes = shared_tree(n_req, page_tables, max_pages, ctx_lens, page_size, SHARED_STAGE / page_size);
+// Most rows of partial results of a plan.  A node leaves one for every token and query head of its run, so deeply nested prefixes would
+// leave as many as there are levels, at (4 head_dim + 8) bytes each (512 requests of 8 tokens and 32 heads of 128, each sharing 128 keys more with the next:
+// 33.7 M rows, 17.6 GB, for an output of 34 MB).  Eight rows an output row are more than two or three levels and the cuts between CTAs
+// ask for; half a million (273 MB with heads of 128) leave room for the parts of few rows on very many keys.
+inline int64_t shared_most_rows(int64_t out_rows) { return std::max<int64_t>((int64_t)1 << 19, 8 * out_rows); }
+
+inline void shared_cut(const std::vector<SharedNode>& nodes, int n_req, const int* chunk_offsets, const int* ctx_lens, int page_size,
+                       int group, int n_kv_heads, int n_sm, const SharedCost& cost, SharedPlan& sp) {
     const int T = chunk_offsets[n_req], tile_tokens = SHARED_TILE_ROWS / group;
     // units: a node's tokens in items of at most two tiles
     struct Unit { int q_tok, n_tok, req, kv_begin, kv_end, q_pos0, tiles, stages; int64_t time; };
@@ -205,6 +210,23 @@ inline void shared_plan(int n_req, const int* chunk_offsets, const int* page_tab
         sp.list[k++] = p.base + off;
         if (p.second >= 0) sp.list[k++] = p.second + off;
     });
+}
+
+// Where the tree of all common prefixes would leave too many rows, a common prefix has to be twice as long to be worth a node, and so
+// on: in the end nothing is shared.
+inline void shared_plan(int n_req, const int* chunk_offsets, const int* page_tables, int max_pages, const int* ctx_lens, int page_size,
+                        int group, int n_kv_heads, int n_sm, const SharedCost& cost, SharedPlan& sp) {
+    const int64_t heads = (int64_t)group * n_kv_heads, most = shared_most_rows(heads * chunk_offsets[n_req]);
+    for (int64_t least = SHARED_STAGE / page_size;; least *= 2) {
+        const std::vector<SharedNode> nodes = shared_tree(n_req, page_tables, max_pages, ctx_lens, page_size, (int)least);
+        const bool leaves_alone = nodes.size() == (size_t)n_req;
+        int64_t rows = 0;   // of one item a node and tile
+        for (const SharedNode& nd : nodes) rows += heads * (chunk_offsets[nd.b] - chunk_offsets[nd.a]);
+        if (rows > most && !leaves_alone) continue;
+        sp = SharedPlan();
+        shared_cut(nodes, n_req, chunk_offsets, ctx_lens, page_size, group, n_kv_heads, n_sm, cost, sp);
+        if (sp.rows <= most || leaves_alone) return;
+    }
 }
 
 }  // namespace syn

@@ -1272,7 +1272,7 @@ static bool shared_better(const syn_model_desc& c, int P, int n_sm, int32_t n_re
                           int32_t max_pages, const int32_t* ctx_lens, const HostPlan& hp, SharedPlan& sp) {
     if (g_attention != 0 && g_attention != ATTN_SHARED) return false;
     shared_plan(n_req, chunk_offsets, page_tables, max_pages, ctx_lens, P, c.n_q_heads / c.n_kv_heads, c.n_kv_heads, n_sm, shared_cost(c), sp);
-    if (sp.rows > (int64_t)1 << 30) return false;
+    if (sp.rows > shared_most_rows((int64_t)chunk_offsets[n_req] * c.n_q_heads)) return false;
     return g_attention == ATTN_SHARED || sp.estimate * 100 < hp.estimate * (sp.shares ? 100 : 85);
 }
 

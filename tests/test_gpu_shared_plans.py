@@ -7,6 +7,7 @@ import torch
 import paper_2511_07423_b200 as syn
 from test_gpu_shared import check, model_of, reference, setup as batch
 from test_shared_plan_host import tree_batch
+from test_shared_plan_rows import staircase
 
 pytestmark = pytest.mark.gpu
 
@@ -53,4 +54,20 @@ def test_room_for_the_partials_but_not_for_the_lists():
     del fill
     torch.cuda.empty_cache()
     check(again.attention(1, q), want, size)
+    assert model.status() == 0
+
+
+def test_nested_prefixes_on_a_coarser_tree():
+    """64 requests of 8 tokens whose common prefixes grow by 128 keys from one to the next: the whole tree would leave 548 608 rows."""
+    n, chunk, hq, hkv, hd = 64, 8, 32, 8, 128
+    table, ctx, n_pages = staircase(n)
+    model = model_of(hd, hq, hkv)
+    kv = syn.KVCache(model, n_pages)
+    pool = kv.layer_view(1)
+    pool.normal_(0, 1, generator=torch.Generator(device="cuda").manual_seed(23))
+    off = torch.arange(n + 1, dtype=torch.int32) * chunk
+    q = torch.empty(n * chunk, hq * hd, dtype=torch.float16, device="cuda").normal_(0, 1.3)
+    plan = syn.Plan(kv, torch.zeros(n * chunk, dtype=torch.int32), off, table, ctx, share_prefix=True)
+    assert plan.attention_kernel() == 4
+    check(plan.attention(1, q), *reference(pool, q, table, ctx, off))
     assert model.status() == 0
