@@ -33,12 +33,14 @@ struct SharedItem {
 enum SharedMode { SHARED_GROUP0 = 0, SHARED_GROUP1 = 1, SHARED_TILES = 2, SHARED_STAGES = 3 };
 constexpr int SHARED_SOLO_STAGES = 4;    // most stages of an item that one group takes alone
 
-// Cycles of an item by its stages, and of a launch with its merge.
+// Cycles of an item by its stages, and of a launch with its merge: where requests share keys, besides for each partial row, which
+// deeply nested prefixes leave many of.
 struct SharedCost {
     int tiles_stage, tiles_item;     // two tiles
     int stages_stage, stages_item;   // one tile, both groups
     int solo_stage, solo_item;       // one tile, one group; the other group's items run beside it
-    int fixed;
+    int fixed;                       // nothing is shared
+    int fixed_shared, row_256;       // (of 256 rows)
     int64_t of(int tiles, int stages) const {
         return tiles == 2 ? (int64_t)stages * tiles_stage + tiles_item
                           : stages <= SHARED_SOLO_STAGES ? (int64_t)stages * solo_stage + solo_item : (int64_t)stages * stages_stage + stages_item;
@@ -167,7 +169,6 @@ inline void shared_cut(const std::vector<SharedNode>& nodes, int n_req, const in
         const int64_t mid = (lo + hi) / 2;
         if (fill(mid, nothing)) hi = mid; else lo = mid;
     }
-    sp.estimate = hi + cost.fixed;
     std::vector<int> owner, solo(n_sm, 0);   // (a CTA's items of one group: the groups in turn)
     // parts of (unit, head), for the lists below
     struct Part { int unit, h, base, second; };
@@ -181,6 +182,7 @@ inline void shared_cut(const std::vector<SharedNode>& nodes, int n_req, const in
         sp.rows += (int64_t)rows * copies;
         owner.push_back(cta);
     });
+    sp.estimate = hi + (sp.shares ? cost.fixed_shared + sp.rows * cost.row_256 / 256 : cost.fixed);
     sp.n_cta = owner.back() + 1;
     sp.cta_begin.assign(sp.n_cta + 1, 0);
     for (int k : owner) sp.cta_begin[k + 1]++;

@@ -1258,16 +1258,18 @@ static int plan_compute(const syn_model_desc& c, int P, uint32_t n_pages, int n_
 // The attention kernel that plans are laid out for unless they share prefixes (0: the planner's choice).
 static int attention_choice() { return g_attention == ATTN_SHARED ? 0 : g_attention; }
 
-// SM cycles of the shared-prefix kernel, fitted to the items' own times in the batches of the 8B and 32B shapes.
+// SM cycles of the shared-prefix kernel, fitted to the items' own times in the batches of the 8B and 32B shapes, and those of a launch to
+// 248 batches: without a cost a partial row the choice lost up to 31 % where prefixes are nested (32 requests, each sharing 128 keys
+// more with the next: 62 us against the plain kernels' 48).
 static SharedCost shared_cost(const syn_model_desc& c) {
-    return c.head_dim == 128 ? SharedCost{3450, 11500, 2550, 4500, 1900, 3600, 14000} : SharedCost{3350, 7500, 2080, 4000, 1700, 3600, 11500};
+    return c.head_dim == 128 ? SharedCost{3450, 11500, 2550, 4500, 1900, 3600, 14000, 11000, 64} : SharedCost{3350, 7500, 2080, 4000, 1700, 3600, 11500, 9500, 48};
 }
 
 // Whether a batch planned as `hp` is better off on the shared-prefix kernel; fills `sp`.  Where nothing is shared that kernel still cuts
 // the keys of a few long requests into more and shorter items (2 requests of 29 589 keys, 16 tokens, 14 heads on 2 of 128: 23 us against 125;
 // one of 20 064, 4 tokens: 13 against 25), and has to be estimated 15 % better there, for the batch is otherwise the plan without
 // sharing, whose results do not depend on this.  Against the better kernel of each batch the choice loses 2.6 % in 48 batches that
-// share nothing (23 % when it kept to the other kernels there; 0.9 % with 8 % for 15), 1.1 % in 120 that do or are one request.
+// share nothing (23 % when it kept to the other kernels there; 0.9 % with 8 % for 15), 0.9 % in 200 that do or are one request.
 static bool shared_better(const syn_model_desc& c, int P, int n_sm, int32_t n_req, const int32_t* chunk_offsets, const int32_t* page_tables,
                           int32_t max_pages, const int32_t* ctx_lens, const HostPlan& hp, SharedPlan& sp) {
     if (g_attention != 0 && g_attention != ATTN_SHARED) return false;

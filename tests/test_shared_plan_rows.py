@@ -45,3 +45,12 @@ def test_prefixes_that_stay_within_the_bound_are_cut_as_finely_as_before():
     p = syn.plan_shared_host(shape(128, 32, 8), n_pages, torch.zeros(128, dtype=torch.int32), torch.arange(17, dtype=torch.int32) * 8, table, ctx)
     shared = {(r[4], r[5]) for r in p["items"].tolist() if r[6] < 0}
     assert {(128 * i, 128 * (i + 1)) for i in range(1, 15)} <= shared     # (the first level's 128 keys are met by all)
+
+
+@pytest.mark.parametrize("n,chunk,taken", [(32, 8, False), (64, 24, False), (64, 8, True), (128, 8, True), (64, 1, True)])
+def test_what_the_merge_costs_counts(n, chunk, taken):
+    """32 requests of 8 tokens leave 143 104 partial rows for 8 192 rows of output: measured 62 us against the plain kernels' 48; 64 of 24
+    tokens 222 against 173.  Single tokens leave few rows, and on the coarser trees of larger batches sharing pays."""
+    table, ctx, n_pages = staircase(n)
+    p = syn.plan_shared_host(shape(128, 32, 8), n_pages, torch.zeros(n * chunk, dtype=torch.int32), torch.arange(n + 1, dtype=torch.int32) * chunk, table, ctx)
+    assert p["taken"] == taken
