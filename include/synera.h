@@ -370,7 +370,8 @@ enum {
 /* Pair i of the rotary_dim leading components of a head turns by pos * f_i, f_i = base^(-2 i / rotary_dim) scaled as above:
  * components (i, i + rotary_dim / 2) in halves, (2 i, 2 i + 1) interleaved; the other components pass through.  amplitude
  * multiplies cosine and sine; 0 stands for 1, and for 0.1 ln(factor) + 1 with SYN_ROPE_SCALE_INDEX.  rotary_dim: even, 2 to
- * 256.  low, high, original_len: for the last two scalings only; factor: for all but the first. */
+ * 256.  low, high, original_len: for the last two scalings only; factor: for all but the first.  Refused besides: a base or an angle
+ * (of a position of 2^31) that leaves the range of 64 bits, an amplitude that leaves that of 32. */
 typedef struct {
     uint32_t rotary_dim, layout, scaling;
     double base, factor, original_len, low, high, amplitude;

@@ -2589,11 +2589,12 @@ extern "C" int syn_rope_create(const syn_rope_desc* desc, syn_rope** out) {
     if ((d.scaling == SYN_ROPE_SCALE_TURNS || d.scaling == SYN_ROPE_SCALE_INDEX) && (!positive(d.original_len) || !positive(d.low) || !std::isfinite(d.high) || d.high <= d.low))
         return SYN_E_INVALID_ARG;
     if (d.scaling == SYN_ROPE_SCALE_INDEX && d.base <= 1.0) return SYN_E_INVALID_ARG;
-    syn_rope* r = new (std::nothrow) syn_rope();
-    if (!r) return SYN_E_OOM;
     const int n = (int)d.rotary_dim / 2;
     const double dim = (double)d.rotary_dim;
     const double base = d.scaling == SYN_ROPE_SCALE_BASE && n > 1 ? d.base * std::pow(d.factor, dim / (dim - 2.0)) : d.base;
+    if (!positive(base)) return SYN_E_INVALID_ARG;   // infinite: no pair but the first would turn
+    syn_rope* r = new (std::nothrow) syn_rope();
+    if (!r) return SYN_E_OOM;
     double first = 0.0, last = 0.0;
     if (d.scaling == SYN_ROPE_SCALE_INDEX) {
         auto index_of = [&](double turns) { return dim * std::log(d.original_len / (turns * 2.0 * PI)) / (2.0 * std::log(d.base)); };
@@ -2609,9 +2610,17 @@ extern "C" int syn_rope_create(const syn_rope_desc* desc, syn_rope** out) {
         keep = std::min(1.0, std::max(0.0, keep));
         r->freq[i] = keep == 1.0 ? f : f * keep + f / d.factor * (1.0 - keep);
         r->table.turns[i] = r->freq[i] / (2.0 * PI);
+        if (!std::isfinite(r->freq[i] * 2147483648.0)) {   // the angle of some position would be none
+            delete r;
+            return SYN_E_INVALID_ARG;
+        }
     }
     r->amplitude = d.amplitude != 0.0 ? d.amplitude : d.scaling == SYN_ROPE_SCALE_INDEX && d.factor > 1.0 ? 0.1 * std::log(d.factor) + 1.0 : 1.0;
     r->table.amplitude = (float)r->amplitude;
+    if (!std::isnormal(r->table.amplitude)) {
+        delete r;
+        return SYN_E_INVALID_ARG;
+    }
     r->table.half = n;
     r->table.interleaved = d.layout == SYN_ROPE_INTERLEAVED;
     r->rotary_dim = (int)d.rotary_dim;
