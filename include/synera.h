@@ -324,7 +324,8 @@ int syn_debug_set_attention(int32_t which);
 /* The ragged paged attention of the step on its own (paper Sec. 3.2 attention equation over a
  * paged cache).  q: DEVICE half precision [T][n_q_heads*head_dim] (rotated); out: DEVICE half
  * precision, same shape.  The plan supplies page tables, lengths and the work list; the chunk's K/V must
- * already be in the pool of `layer`.  Asynchronous on cuda_stream. */
+ * already be in the pool of `layer`.  out must be aligned to 16 bytes where syn_plan_attention is 2, to 8 elsewhere
+ * (SYN_E_INVALID_ARG).  Asynchronous on cuda_stream. */
 int syn_op_attention(syn_model *m, syn_kv *kv, const syn_plan *p, uint32_t layer, const void *q, void *out,
                      void *cuda_stream);
 

@@ -503,11 +503,20 @@ class Plan:
             _check(code, "syn_op_kv_append")
         return q_out if q is not None else None
 
+    def _attention_operands(self, q: torch.Tensor, out: Optional[torch.Tensor], stream) -> torch.Tensor:
+        assert q.is_cuda and q.dtype == torch.float16 and q.is_contiguous()
+        n = self.n_tokens * self.kv.model.shape.q_dim
+        if q.numel() < n:
+            raise SynError(-1, f"attention: q of {n} elements")
+        if out is None:
+            return _empty(q.shape, q.dtype, q.device, stream)
+        if out.dtype is not torch.float16 or out.numel() < n or not out.is_contiguous() or out.get_device() != q.get_device():
+            raise SynError(-1, f"attention: a contiguous float16 result of {n} elements on the queries' device")
+        return out
+
     def attention(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """syn_op_attention: q and the result are half precision [T, n_q_heads * head_dim]."""
-        assert q.is_cuda and q.dtype == torch.float16 and q.is_contiguous()
-        if out is None:
-            out = _empty(q.shape, q.dtype, q.device, stream)
+        out = self._attention_operands(q, out, stream)
         _check(self._lib.syn_op_attention(self.kv.model._h, self.kv._h, self._h, C.c_uint32(layer),
                                           C.c_void_p(q.data_ptr()), C.c_void_p(out.data_ptr()), _stream_ptr(stream)),
                "syn_op_attention")
@@ -524,9 +533,7 @@ class Plan:
         """syn_op_attention_static: the attention of the step for callers that cannot allocate while
         they run; its partial results live in a fixed array inside the library.  Pass `out` to keep
         the call itself free of allocations on the Python side too."""
-        assert q.is_cuda and q.dtype == torch.float16 and q.is_contiguous()
-        if out is None:
-            out = _empty(q.shape, q.dtype, q.device, stream)
+        out = self._attention_operands(q, out, stream)
         _check(self._lib.syn_op_attention_static(self.kv.model._h, self.kv._h, self._h, C.c_uint32(layer),
                                                  C.c_void_p(q.data_ptr()), C.c_void_p(out.data_ptr()),
                                                  _stream_ptr(stream)), "syn_op_attention_static")

@@ -2491,6 +2491,9 @@ extern "C" int syn_debug_linear_counter(int32_t index, int32_t value) {
     return SYN_OK;
 }
 
+// Whether the attention kernel of a plan can store to `out`: four, eight or sixteen bytes at a time.
+static bool attention_out_ok(const syn_plan* p, const void* out) { return ((uintptr_t)out & (p->attn == ATTN_TENSOR ? 15 : 7)) == 0; }
+
 static int syn_op_attention_impl(syn_model* m, syn_kv* kv, const syn_plan* p, uint32_t layer, const void* q, void* out,
                                 void* cuda_stream) {
     if (!m || !kv || !p || kv->model != m || !plan_matches(p, kv) || !q || !out || layer >= m->desc.n_layers)
@@ -2498,8 +2501,9 @@ static int syn_op_attention_impl(syn_model* m, syn_kv* kv, const syn_plan* p, ui
     const syn_model_desc& c = m->desc;
     const int q_dim = c.n_q_heads * c.head_dim;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    if (!attention_out_ok(p, out)) return SYN_E_INVALID_ARG;
     if (p->attn == ATTN_SHARED) {   // reads the caller's q where it is
-        if (((uintptr_t)q & 15) || ((uintptr_t)out & 7)) return SYN_E_INVALID_ARG;
+        if ((uintptr_t)q & 15) return SYN_E_INVALID_ARG;
         return launch_shared(m, kv, p, layer, (const op16*)q, (op16*)out, st);
     }
     if (p->T > m->t_cap || p->n_parts > m->part_cap) return SYN_E_INVALID_ARG;
@@ -2551,6 +2555,7 @@ static int syn_op_attention_static_impl(syn_model* m, syn_kv* kv, const syn_plan
     if (!m || !kv || !p || kv->model != m || !plan_matches(p, kv) || !q || !out || layer >= m->desc.n_layers)
         return SYN_E_INVALID_ARG;
     if (p->attn == ATTN_SHARED) return syn_op_attention_impl(m, kv, p, layer, q, out, cuda_stream);   // its partials are the plan's
+    if (!attention_out_ok(p, out)) return SYN_E_INVALID_ARG;
     const syn_model_desc& c = m->desc;
     const int q_dim = c.n_q_heads * c.head_dim;
     if (p->T > m->t_cap) return SYN_E_INVALID_ARG;
