@@ -598,17 +598,16 @@ shared_merge_kernel(SharedParams p, int n_rows_out) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u < n) load(u, v[u]);                         // on their way while the weights are made
-        // A part in which the row sees nothing (its sum is zero) has no say.  Every other counts even where its weight is zero: a sum or
-        // a result that is no number (maybe its reference exponent too) stays none.
+        // A part in which the row sees nothing (its sum is zero) has no say: the weight of -1 tells.  Every other counts even where its
+        // weight is zero: a sum or a result that is no number (maybe its reference exponent too) stays none.
         const bool say = ml.y != 0.f;
-        const uint32_t says = __ballot_sync(0xFFFFFFFFu, say);
         const float mk = say ? ml.x : -INFINITY;
         float mn = mk;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, o));
         mn = fmaxf(m, mn);
         const float bs = mn == -INFINITY ? 0.f : mn, corr = ex2_approx(m - bs);
-        const float w = ex2_approx(mk - bs);
+        const float w = say ? ex2_approx(mk - bs) : -1.f;
         float ws = w * ml.y;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) ws += __shfl_xor_sync(0xFFFFFFFFu, ws, o);
@@ -622,7 +621,7 @@ shared_merge_kernel(SharedParams p, int n_rows_out) {
                 if (k + u >= n) break;
                 const float wk = __shfl_sync(0xFFFFFFFFu, w, (k + u) & 31);
 #pragma unroll
-                for (int i = 0; i < E; ++i) acc[i] = says >> ((k + u) & 31) & 1u ? fmaf(v[u][i], wk, acc[i]) : acc[i];
+                for (int i = 0; i < E; ++i) acc[i] = wk < 0.f ? acc[i] : fmaf(v[u][i], wk, acc[i]);
             }
             k += U;
             if (k >= n) break;

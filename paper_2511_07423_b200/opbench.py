@@ -17,7 +17,8 @@ reports the iterations by kind and the share of the wall time spent in the sched
 `sample` times the sampling-verification stage (top-k of the logits rows + the per-request kernel)
 behind a one-layer model with the configuration's vocabulary and request mix.
 `prefix` times the attention of a batch whose requests share a prefix: the chosen configuration's heads and chunks, `--shared` common
-tokens and `--own` cached tokens of each request, with every request's keys read by itself and with the shared ones met once.
+tokens and `--own` cached tokens of each request, with every request's keys read by itself and with the shared ones met once, and
+(plan_ms) making a plan and letting it go, which a batch pays once for all its layers.
 `rope` times the per-head norm and rotation of queries and keys, and their append to the cache.
 `scale` is the scalability experiment of the paper's Sec. 6.4 in shape: the arrival-driven workload
 of workloads/arrivals.py (sessions arrive at a given rate, every device drafts chunks of gamma tokens
@@ -31,6 +32,7 @@ from __future__ import annotations
 import argparse
 import dataclasses
 import json
+import time
 
 import torch
 
@@ -127,9 +129,16 @@ def bench_prefix(a):
     out = torch.empty_like(q)
     line = {"op": "prefix", "config": wl.name, "n_req": n, "T": T, "shared": common * 16, "own": a.own}
     for name, share in (("each", False), ("shared", True)):
-        plan = syn.Plan(kv, torch.zeros(T, dtype=torch.int32), batch.chunk_offsets, table, ctx, share_prefix=share)
+        make = lambda: syn.Plan(kv, torch.zeros(T, dtype=torch.int32), batch.chunk_offsets, table, ctx, share_prefix=share)  # noqa: E731
+        plan = make()
         med, best = _time(lambda: plan.attention(0, q, out), a.iters)
         st = plan.stats()
+        walls = []
+        for _ in range(9):   # what a new batch pays besides: its plan made and let go
+            t0 = time.perf_counter()
+            make().close()
+            walls.append(time.perf_counter() - t0)
+        line[f"{name}_plan_ms"] = sorted(walls)[len(walls) // 2] * 1e3
         line.update({f"{name}_kernel": plan.attention_kernel(), f"{name}_ms": med, f"{name}_kv_bytes": st.kv_read_bytes, f"{name}_tflops": st.attn_flops / med / 1e9})
     assert model.status() == 0
     print(json.dumps(line))
@@ -160,7 +169,6 @@ def bench_rope(a):
 
 
 def bench_sched(a):
-    import time
     wl = CONFIGS[a.config]
     shape = wl.shape
     model = synthetic.load_model(shape, wl.seed)
@@ -246,7 +254,6 @@ def bench_sample(a):
 
 
 def bench_scale(a):
-    import time
     from workloads import arrivals
     wl = CONFIGS[a.config]
     shape = wl.shape
