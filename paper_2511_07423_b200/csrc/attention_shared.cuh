@@ -17,13 +17,15 @@
 // MMAs of a group each, warps 4..7 and 8..11 are the softmax groups.  tcgen05 operations of one thread complete in order, and a
 // commit tells that all before it are done.  The maximum that P is relative to is raised only when a half stage exceeds it by 2^8; P is
 // scaled by 2^7 besides (at most 2^15 in half precision, so that weights down to 2^-21 of the largest keep all their bits).
-// Every wait is bounded.
+// Every wait on a barrier in shared memory is bounded.  The turns are named barriers, which are not: a wait that has run out takes the work out of
+// a group's loop but leaves its turns, so both groups meet on them equally often whatever has failed.
 //
 // What bounds it, on an 8B-shaped layer (32 query and 8 kv heads of 128): with two tiles a stage takes 3 430 cycles where the tensor
 // cores need 2 048 and the exponentials (16 a cycle) 2 048 too; a group's warps, one to a scheduler, wait for the latencies of
 // their own instructions, 860 cycles a half stage for the exponentials alone, which the two groups take in turns (shr_turn).  Above about
-// 900 TFLOP/s the power cap takes back what cycles are saved (1.6 GHz).  256 requests of 8 tokens on 12 016 shared keys: 409 us, 996 TFLOP/s
-// (24 chunks of 32 on 32 768 keys: 404 us, 1 035).  With one tile the keys' bytes: three requests on 131 072 keys 93 us, 5.8 TB/s.
+// 900 TFLOP/s the power cap takes back what cycles are saved (1.6 GHz).  256 requests of 8 tokens on 12 016 shared keys: 413 us, 986 TFLOP/s
+// (24 chunks of 32 on 32 768 keys: 407 us, 1 027).  With one tile the keys' bytes: three requests on 131 072 keys 94 us, 5.7 TB/s.  These are
+// times in a graph of 20 launches with their merges; a row of calls without pause takes 483, 479 and 107 us, at the power cap's clocks.
 // Tried and slower (256 requests): P over S in shared columns with 128-key stages 490 us, one issuer for both groups 571; exponentials
 // not in turns 4 230 cycles a stage; a quarter of them by a polynomial on the multiply-add units 3 780; no maximum but a check of
 // the sum 4 800; the next half stage's scores fetched before this one's exponentials 750 us.
@@ -546,8 +548,9 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 }
 
 // Joins the partials of a (token, query head): WPR warps take its parts in turn.  The lanes of a warp read 32 parts' (m, l) at a
-// time, then O part by part, four on their way at once (eight where a block has one row: there the parts are many and the warps few).  Which rows belong together is the plan's, so it is looked up before
-// the predecessor's results are waited for.
+// time, then O part by part, four on their way at once (eight where a block has one row: there the parts are many and the warps few).
+// Which rows belong together is the plan's, so it is looked up before the predecessor's results are waited for.  Measured: 37 us for 131 072
+// partial rows of 128 (68 MB, 1.8 TB/s): latency, with 40 registers for 12 blocks an SM (and 40 bytes spilled) and four loads a warp.
 constexpr int SHR_MERGE_SPLIT_ROWS = 16;   // rows an SM from which on a warp takes one alone
 template <int HD, int WPR>
 __global__ void __launch_bounds__(128, WPR > 1 ? 1 : 12)

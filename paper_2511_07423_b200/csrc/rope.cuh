@@ -14,6 +14,8 @@
 // tokens in fp32 30.6 us = 5.5 TB/s.  In 16 bits instruction issue is as near its bound as HBM: the arithmetic runs on pairs of values
 // (with single ones 52 us), gains are multiplied into the cosines and sines (integer divisions, a barrier per token and a table
 // for several tokens had it at 71).  A half that is no multiple of 4 components (54 of 128: 81 us) is read one by one.
+// The launch bounds hold an instance to 64 registers (40 with one access in flight), and each spills: in bf16 40 bytes of stores in halves, 80
+// in pairs, 400 one by one.
 #pragma once
 #include "ptx.cuh"
 
